@@ -173,6 +173,39 @@ ps_status ps_kv_create(const ps_layer_cfg* cfg, int32_t n_layers, int32_t n_page
                        int32_t max_pages_per_seq, void* pool, uint64_t page_order_seed, ps_kv** out);
 ps_status ps_kv_destroy(ps_kv* kv);
 
+/* The same pool with keys and values held in 8 bits: e4m3 (OCP: largest 448, no
+ * infinities) with a scale for each (layer, page, KV head) and keys or values, a
+ * power of two. Half the bytes of a bf16 pool, so twice the tokens and half the
+ * attention traffic of a decode step (§III-C, Observation 3: decode concurrency
+ * is bounded by the bytes each token pins). For bf16 layers with head_dim 64 or
+ * 128 and any n_q_heads / n_kv_heads (else PS_E_UNSUPPORTED). The handle is a
+ * ps_kv like any other: every call that takes one works on it (ps_kv_*,
+ * ps_sched_*, ps_op_rope_kvwrite, ps_op_attention, ps_op_decode_*, the layer and
+ * model calls, with the same arguments and workspace bounds), except that
+ * ps_kv_transfer needs both pools stored alike. Activations stay bf16: ps_kv_append
+ * takes and ps_kv_gather returns bf16 rows.
+ *
+ * What is stored. Writing tokens into a page: e = the smallest integer in [-100,
+ * 119] with |x| <= 448 2^e for all finite x among the new tokens' keys (or
+ * values) of the page and head, and where the page holds earlier tokens of the
+ * sequence at least their exponent. A value is held as x 2^-e rounded to e4m3
+ * (nearest, ties to even, values past 448 2^119 to that); an infinity or NaN is
+ * held as NaN. Where e grows, the earlier tokens' bytes are rounded anew to the
+ * larger scale; all such roundings together stay below one step of the last. A
+ * page's content therefore depends on how its tokens were grouped into calls
+ * only by those roundings. Keys are rotated in fp32 before they are rounded.
+ * Attention reads byte * 2^e, which is exact in bf16.
+ *
+ * Device layout of the pool (ps_kv8_pool_bytes bytes): blocks
+ *   [n_layers][n_pages][n_kv][ K: 16 hd bytes | V: 16 hd bytes ]
+ *   K: [hd / 16][16 tokens][16 dims]
+ *   V: [hd / 64][token / 4][dim % 16][dim % 64 / 16][token % 4]
+ * then the scales 2^e as fp32 [n_layers][n_kv][n_pages][2] (K, V). The contents
+ * need no initial value. */
+size_t ps_kv8_pool_bytes(const ps_layer_cfg* cfg, int32_t n_layers, int32_t n_pages);
+ps_status ps_kv8_create(const ps_layer_cfg* cfg, int32_t n_layers, int32_t n_pages, int32_t max_seqs,
+                        int32_t max_pages_per_seq, void* pool, uint64_t page_order_seed, ps_kv** out);
+
 /* Host-only metadata calls. ps_kv_alloc is the per-request, per-stage KV
  * reservation in tokens (the "KV chunk size" CS_i of §III-B's design-space
  * table and §IV-A: CS_T for think, CS_A for answer); PS_E_NO_PAGES when the

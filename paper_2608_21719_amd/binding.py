@@ -98,6 +98,8 @@ _SIGS = {
     "ps_op_tile_weight": (_I, [_I, _I, _I, _P, _P, _P]),
     "ps_kv_pool_bytes": (c_size_t, [POINTER(LayerCfg), _I, _I]),
     "ps_kv_create": (_I, [POINTER(LayerCfg), _I, _I, _I, _I, _P, c_uint64, POINTER(c_void_p)]),
+    "ps_kv8_pool_bytes": (c_size_t, [POINTER(LayerCfg), _I, _I]),
+    "ps_kv8_create": (_I, [POINTER(LayerCfg), _I, _I, _I, _I, _P, c_uint64, POINTER(c_void_p)]),
     "ps_kv_destroy": (_I, [_P]),
     "ps_kv_seq_open": (_I, [_P, _IP]),
     "ps_kv_alloc": (_I, [_P, _I, _I]),
@@ -248,10 +250,13 @@ class KV:
         self.cfg = cfg
         self.n_layers = n_layers
         self.pool = pool  # keep the owner alive
+        self.h = None
         h = c_void_p()
-        check(lib.ps_kv_create(ctypes.byref(cfg), n_layers, n_pages, max_seqs, max_pages_per_seq, ptr(pool),
-                               c_uint64(seed), ctypes.byref(h)))
+        check(self._create(ctypes.byref(cfg), n_layers, n_pages, max_seqs, max_pages_per_seq, ptr(pool),
+                           c_uint64(seed), ctypes.byref(h)))
         self.h = h
+
+    _create = staticmethod(lib.ps_kv_create)
 
     @staticmethod
     def pool_bytes(cfg: LayerCfg, n_layers: int, n_pages: int) -> int:
@@ -314,6 +319,16 @@ class KV:
     def gather(self, layer, seq, k_out, v_out, ws, stream=None):
         check(lib.ps_kv_gather(self.h, layer, seq, ptr(k_out), ptr(v_out), ptr(ws),
                                ws.numel() * ws.element_size(), stream_handle(stream)))
+
+
+class KV8(KV):
+    """A KV pool held in e4m3 with a power-of-two scale per page, head, and keys or values."""
+
+    _create = staticmethod(lib.ps_kv8_create)
+
+    @staticmethod
+    def pool_bytes(cfg: LayerCfg, n_layers: int, n_pages: int) -> int:
+        return lib.ps_kv8_pool_bytes(ctypes.byref(cfg), n_layers, n_pages)
 
 
 def kv_transfer(src: KV, src_seq: int, dst: KV, dst_seq: int, ws, stream=None):

@@ -217,11 +217,16 @@ struct ps_kv {
   KvPool meta;
   Staging staging;
   DecodeAttnPlan dplan;
-  ps_kv(const ps_layer_cfg& c, int32_t nl, int32_t np, int32_t ms, int32_t mp, void* p, uint64_t seed)
+  bool e4m3;  // 8-bit storage (kv8.h): blocks of all layers, then the scales
+  ps_kv(const ps_layer_cfg& c, int32_t nl, int32_t np, int32_t ms, int32_t mp, void* p, uint64_t seed, bool e4m3_ = false)
       : cfg(c), n_layers(nl), pool(p),
-        layer_elts((size_t)np * c.n_kv_heads * 2 * PS_PAGE_TOKENS * c.head_dim), meta(np, ms, mp, seed) {}
-  void* layer_base(int layer) const {
-    return (char*)pool + (size_t)layer * layer_elts * elt_bytes(cfg.dtype);
+        layer_elts((size_t)np * c.n_kv_heads * 2 * PS_PAGE_TOKENS * c.head_dim), meta(np, ms, mp, seed), e4m3(e4m3_) {}
+  size_t layer_bytes() const { return layer_elts * (e4m3 ? 1 : elt_bytes(cfg.dtype)); }
+  void* layer_base(int layer) const { return (char*)pool + (size_t)layer * layer_bytes(); }
+  size_t layer_scales() const { return (size_t)cfg.n_kv_heads * meta.n_pages(); }
+  Kv8Layer layer8(int layer) const {
+    return Kv8Layer{(uint8_t*)layer_base(layer), (float2*)layer_base(n_layers) + (size_t)layer * layer_scales(),
+                    meta.n_pages()};
   }
 };
 
@@ -376,6 +381,27 @@ extern "C" ps_status ps_kv_create(const ps_layer_cfg* c, int32_t n_layers, int32
   if (!pool) return fail(PS_E_INVALID, "null pool");
   if (ps_status rc = check_aligned({pool})) return rc;
   *out = new ps_kv(*c, n_layers, n_pages, max_seqs, max_pages_per_seq, pool, seed);
+  return PS_OK;
+  PS_CATCH
+}
+
+extern "C" size_t ps_kv8_pool_bytes(const ps_layer_cfg* c, int32_t n_layers, int32_t n_pages) {
+  if (!c || n_layers <= 0 || n_pages <= 0) return 0;
+  return (size_t)n_layers * n_pages * c->n_kv_heads * (2 * PS_PAGE_TOKENS * c->head_dim + sizeof(float2));
+}
+
+extern "C" ps_status ps_kv8_create(const ps_layer_cfg* c, int32_t n_layers, int32_t n_pages, int32_t max_seqs,
+                                   int32_t max_pages_per_seq, void* pool, uint64_t seed, ps_kv** out) {
+  PS_TRY
+  if (ps_status rc = check_cfg(c)) return rc;
+  if (!out) return fail(PS_E_INVALID, "null out");
+  if (c->dtype != PS_BF16) return fail(PS_E_UNSUPPORTED, "an e4m3 KV pool serves bf16 layers");
+  if (c->head_dim != 64 && c->head_dim != 128) return fail(PS_E_UNSUPPORTED, "an e4m3 KV pool takes head_dim 64 or 128");
+  if (n_layers <= 0 || n_pages <= 0 || max_seqs <= 0 || max_pages_per_seq <= 0)
+    return fail(PS_E_INVALID, "non-positive pool size");
+  if (!pool) return fail(PS_E_INVALID, "null pool");
+  if (ps_status rc = check_aligned({pool})) return rc;
+  *out = new ps_kv(*c, n_layers, n_pages, max_seqs, max_pages_per_seq, pool, seed, true);
   return PS_OK;
   PS_CATCH
 }
@@ -827,6 +853,7 @@ size_t fa_part_ml_bytes(int n_q) { return (size_t)fa_query_tile() * n_q * 2 * si
 
 bool use_mfma_attn(const ps_layer_cfg& c) { return c.dtype == PS_BF16 && c.head_dim == 128; }
 int group_of(const ps_layer_cfg& c) { return c.n_q_heads / c.n_kv_heads; }
+int fa_groups(const ps_layer_cfg& c) { return c.n_kv_heads * ((group_of(c) + 3) / 4); }  // workgroups per query tile
 bool fa_ok(const ps_layer_cfg& c) { return use_mfma_attn(c) && group_of(c) % 4 == 0 && group_of(c) <= 64; }
 bool dec_ok(const ps_layer_cfg& c) {
   const int g = group_of(c);
@@ -953,8 +980,12 @@ extern "C" ps_status ps_kv_append(ps_kv* kv, int32_t layer, int32_t n_seqs, cons
   hipStream_t st = (hipStream_t)stream;
   if (ps_status rc = kv->staging.submit(slot, ws, mt.buf.size(), st)) return rc;
   char* w = (char*)ws;
-  launch_kv_append(kv->cfg.dtype, cs.rows, k, v, kv->layer_base(layer), (const SeqInfo*)(w + o_si),
-                   (const int32_t*)(w + o_bt), n_seqs, kv->cfg.n_kv_heads, kv->cfg.head_dim, st);
+  if (kv->e4m3)
+    launch_kv8_append(cs.rows, k, v, kv->layer8(layer), (const SeqInfo*)(w + o_si), (const int32_t*)(w + o_bt), n_seqs,
+                      kv->cfg.n_kv_heads, kv->cfg.head_dim, st);
+  else
+    launch_kv_append(kv->cfg.dtype, cs.rows, k, v, kv->layer_base(layer), (const SeqInfo*)(w + o_si),
+                     (const int32_t*)(w + o_bt), n_seqs, kv->cfg.n_kv_heads, kv->cfg.head_dim, st);
   return last_launch_error();
   PS_CATCH
 }
@@ -979,8 +1010,11 @@ extern "C" ps_status ps_kv_gather(ps_kv* kv, int32_t layer, int32_t seq, void* k
   std::memcpy(host, mt.buf.data(), mt.buf.size());
   hipStream_t st = (hipStream_t)stream;
   if (ps_status rc = kv->staging.submit(slot, ws, mt.buf.size(), st)) return rc;
-  launch_kv_gather(kv->cfg.dtype, q.len, kv->layer_base(layer), (const int32_t*)ws, k_out, v_out,
-                   kv->cfg.n_kv_heads, kv->cfg.head_dim, st);
+  if (kv->e4m3)
+    launch_kv8_gather(q.len, kv->layer8(layer), (const int32_t*)ws, k_out, v_out, kv->cfg.n_kv_heads, kv->cfg.head_dim, st);
+  else
+    launch_kv_gather(kv->cfg.dtype, q.len, kv->layer_base(layer), (const int32_t*)ws, k_out, v_out,
+                     kv->cfg.n_kv_heads, kv->cfg.head_dim, st);
   return last_launch_error();
   PS_CATCH
 }
@@ -994,6 +1028,7 @@ extern "C" ps_status ps_kv_transfer(ps_kv* src, int32_t src_seq, ps_kv* dst, int
   PS_TRY
   if (!src || !dst) return fail(PS_E_INVALID, "null kv handle");
   if (!same_cfg(src->cfg, dst->cfg)) return fail(PS_E_INVALID, "source and destination pool configurations differ");
+  if (src->e4m3 != dst->e4m3) return fail(PS_E_INVALID, "source and destination pools store keys and values differently");
   if (src->n_layers != dst->n_layers) return fail(PS_E_INVALID, "source and destination pools differ in layer count");
   std::string e;
   if (int rc = src->meta.check_open(src_seq, e)) return fail(rc, "source: " + e);
@@ -1011,12 +1046,16 @@ extern "C" ps_status ps_kv_transfer(ps_kv* src, int32_t src_seq, ps_kv* dst, int
     hipStream_t st = (hipStream_t)stream;
     if (ps_status rc = upload_meta(dst, mt, ws, st)) return rc;
     const ps_layer_cfg& c = src->cfg;
-    const size_t eb = elt_bytes(c.dtype);
+    const size_t eb = src->e4m3 ? 1 : elt_bytes(c.dtype);
     const size_t page_bytes = (size_t)c.n_kv_heads * 2 * PS_PAGE_TOKENS * c.head_dim * eb;
-    if (launch_kv_copy_pages(page_bytes, pages, src->n_layers, src->pool, src->layer_elts * eb,
-                             (const int32_t*)((char*)ws + o_sb), dst->pool, dst->layer_elts * eb,
+    if (launch_kv_copy_pages(page_bytes, pages, src->n_layers, src->pool, src->layer_bytes(),
+                             (const int32_t*)((char*)ws + o_sb), dst->pool, dst->layer_bytes(),
                              (const int32_t*)((char*)ws + o_db), st))
       return fail(PS_E_UNSUPPORTED, "page copy configuration not supported");
+    if (src->e4m3)
+      launch_kv8_copy_scales(src->layer8(0).scales, src->meta.n_pages(), (const int32_t*)((char*)ws + o_sb),
+                             dst->layer8(0).scales, dst->meta.n_pages(), (const int32_t*)((char*)ws + o_db), pages,
+                             src->n_layers * c.n_kv_heads, st);
     if (ps_status rc = last_launch_error()) return rc;
   }
   // the copied positions become the destination's committed length
@@ -1222,6 +1261,7 @@ FaRoom fa_layer_parts(const ps_layer_cfg& c, int32_t chunk_rows, const GemmRoom&
 struct LayerPlan {
   int32_t rows = 0, chunk_rows = 0, n_chunk = 0, n_dec = 0;
   bool fa = false, dec_mfma = false, full_pages = false;
+  bool kv8 = false;  // the pool is an e4m3 one
   size_t o_si = 0, o_bt = 0, o_fr = 0, o_pi = 0, o_di = 0, o_pb = 0, o_pc = 0;
   int n_pitems = 0, n_ditems = 0;
   int n_merges = 0;  // > 0: the prefill items are split ones
@@ -1260,12 +1300,13 @@ ps_status plan_layer(const ps_layer_cfg& c, const SplitGemms& split, const ps_kv
   P.o_bt = P.mt.add(cs.bt.data(), cs.bt.size() * 4);
   const std::vector<double> fr = inv_freq(c);
   P.o_fr = P.mt.add(fr.data(), fr.size() * 8);
-  P.fa = fa_ok(c) && n_chunk > 0;
-  P.dec_mfma = dec_ok(c) && n_dec > 0;
+  P.kv8 = kv->e4m3;
+  P.fa = (P.kv8 || fa_ok(c)) && n_chunk > 0;
+  P.dec_mfma = (P.kv8 || dec_ok(c)) && n_dec > 0;
   if (P.fa) {
     PrefillSplit sp;
     if (may_split)
-      sp = plan_prefill_split(cs.si, n_chunk, c.n_kv_heads * (group_of(c) / 4), c.n_q_heads, [&] {
+      sp = plan_prefill_split(cs.si, n_chunk, fa_groups(c), c.n_q_heads, [&] {
         P.fa_room = fa_layer_parts(c, P.chunk_rows, P.gemm);
         return P.fa_room.parts;
       });
@@ -1281,7 +1322,7 @@ ps_status plan_layer(const ps_layer_cfg& c, const SplitGemms& split, const ps_kv
     }
   }
   if (P.dec_mfma) {
-    DecodePlan dp = plan_decode(cs.si, n_chunk, choose_split_pages(cs.si, n_chunk, c.n_kv_heads, n_chunk == 0));
+    DecodePlan dp = plan_decode(cs.si, n_chunk, choose_split_pages(cs.si, n_chunk, c.n_kv_heads, n_chunk == 0 && !P.kv8));
     if ((long)dp.items.size() > kMaxDecodeItems)
       return fail(PS_E_UNSUPPORTED, "decode batch exceeds 65535 attention work items");
     P.n_ditems = (int)dp.items.size();
@@ -1341,9 +1382,12 @@ bool mixed_forks(const ps_layer_cfg& c, int32_t chunk_rows, int32_t n_dec) {
 // The kernels of one layer: x_in -> x_out for the planned rows.
 // `up`, if given, is the call's metadata upload: the first kernel carries it
 // (every kernel that reads the metadata runs after that one).
-int launch_layer(const ps_layer_cfg& c, const LayerPlan& P, const ps_layer_w* w, void* pool, const void* x_in,
-                 void* x_out, char* W, hipStream_t st, const UploadJob* up = nullptr, AuxStream* aux = nullptr) {
+int launch_layer(const ps_layer_cfg& c, const LayerPlan& P, const ps_layer_w* w, const ps_kv* kv, int layer,
+                 const void* x_in, void* x_out, char* W, hipStream_t st, const UploadJob* up = nullptr,
+                 AuxStream* aux = nullptr) {
   const WsLayout& wl = P.wl;
+  void* pool = kv->layer_base(layer);
+  const Kv8Layer pool8 = P.kv8 ? kv->layer8(layer) : Kv8Layer{};
   const int d = c.hidden, dq = c.n_q_heads * c.head_dim, dkv = c.n_kv_heads * c.head_dim;
   const int dt = c.dtype, G = group_of(c), rows = P.rows;
   const SeqInfo* si = (const SeqInfo*)(W + P.o_si);
@@ -1370,7 +1414,7 @@ int launch_layer(const ps_layer_cfg& c, const LayerPlan& P, const ps_layer_w* w,
   // round gains (8B, us: one sequence 99.5 -> 96.1, 16 of 1000 tokens 110.2 ->
   // 106.2) and several rounds lose (64 of 1024 to 4096 214 -> 218, 256 of 512
   // to 2048 401 -> 412).
-  const bool rope_in_attn = P.dec_mfma && P.n_chunk == 0 && (long)P.n_ditems * c.n_kv_heads <= 2L * compute_units();
+  const bool rope_in_attn = !P.kv8 && P.dec_mfma && P.n_chunk == 0 && (long)P.n_ditems * c.n_kv_heads <= 2L * compute_units();
   DecodeRope rope;
   // fp32: the norms ride in the GEMMs that read them where their arrangement is
   // the small one, and a pure decode step's RoPE and KV write in its attention.
@@ -1438,10 +1482,19 @@ int launch_layer(const ps_layer_cfg& c, const LayerPlan& P, const ps_layer_w* w,
   auto prefill_attn = [&](hipStream_t s) {
     if (P.fa && P.n_merges > 0) {
       const FaRoom& room = P.fa_room;
-      bad |= launch_fa_prefill_split(G, P.n_pitems, P.n_merges, c.n_kv_heads, qr, pool, si, bt,
-                                     (const PrefillSplitItem*)(W + P.o_pi), (const PrefillMerge*)(W + P.o_mg),
-                                     FaPartials{{(float*)h, (float*)m, (float*)gws}, {room.end[0], room.end[1]}, (float*)xn}, o, scale_log2, s);
-    } else if (P.fa)
+      const FaPartials parts{{(float*)h, (float*)m, (float*)gws}, {room.end[0], room.end[1]}, (float*)xn};
+      const PrefillSplitItem* items = (const PrefillSplitItem*)(W + P.o_pi);
+      const PrefillMerge* merges = (const PrefillMerge*)(W + P.o_mg);
+      if (P.kv8)
+        bad |= launch_kv8_prefill_split(G, c.head_dim, P.n_pitems, P.n_merges, c.n_kv_heads, qr, pool8, si, bt, items, merges,
+                                        parts, o, scale_log2, s);
+      else
+        bad |= launch_fa_prefill_split(G, P.n_pitems, P.n_merges, c.n_kv_heads, qr, pool, si, bt, items, merges, parts, o,
+                                       scale_log2, s);
+    } else if (P.kv8)
+      bad |= launch_kv8_prefill(G, c.head_dim, P.n_pitems, c.n_kv_heads, qr, pool8, si, bt, (const PrefillItem*)(W + P.o_pi),
+                                o, scale_log2, s);
+    else if (P.fa)
       bad |= launch_fa_prefill(G, P.n_pitems, c.n_kv_heads, qr, pool, si, bt, (const PrefillItem*)(W + P.o_pi), o,
                                scale_log2, s);
     else
@@ -1452,6 +1505,12 @@ int launch_layer(const ps_layer_cfg& c, const LayerPlan& P, const ps_layer_w* w,
     if (P.dec_mfma) {
       const char* qd = qr + (size_t)P.chunk_rows * dq * eb;
       char* od = o + (size_t)P.chunk_rows * dq * eb;
+      if (P.kv8) {
+        bad |= launch_kv8_decode(G, c.head_dim, P.n_ditems, c.n_kv_heads, P.n_dec, qd, pool8, si + P.n_chunk, bt,
+                                 (const DecodeItem*)(W + P.o_di), (float*)(W + wl.apart_o), (float*)(W + wl.apart_ml),
+                                 (const int32_t*)(W + P.o_pb), (const int32_t*)(W + P.o_pc), od, scale_log2, s, max_wg);
+        return;
+      }
       bad |= launch_decode_attn(G, P.n_ditems, c.n_kv_heads, P.n_dec, qd, pool, si + P.n_chunk, bt,
                                 (const DecodeItem*)(W + P.o_di), (float*)(W + wl.apart_o), (float*)(W + wl.apart_ml),
                                 (const int32_t*)(W + P.o_pb), (const int32_t*)(W + P.o_pc), od, scale_log2, s,
@@ -1483,6 +1542,9 @@ int launch_layer(const ps_layer_cfg& c, const LayerPlan& P, const ps_layer_w* w,
     rope.splits = s_qkv;
     rope.mn = (long)rows * (dq + 2 * dkv);
     rope.inv_freq = (const double*)(W + P.o_fr);
+  } else if (P.kv8) {
+    bad |= launch_kv8_rope_write(rows, qkv, qr, pool8, si, bt, (const double*)(W + P.o_fr), P.n_seqs, c.n_q_heads,
+                                 c.n_kv_heads, c.head_dim, st, (const float*)gws, s_qkv);
   } else if (!f32_rope) {
     bad |= launch_rope_kvwrite(dt, rows, qkv, qr, pool, si, bt, (const double*)(W + P.o_fr), P.n_seqs, c.n_q_heads,
                                c.n_kv_heads, c.head_dim, P.full_pages, st, (const float*)gws, s_qkv);
@@ -1578,7 +1640,7 @@ ps_status run_layer(ps_layer* L, const ps_layer_w* w, ps_kv* kv, int32_t layer, 
     if (ps_status rc = L->aux.get(st, &aux)) return rc;
   UploadJob up;
   if (ps_status rc = stage_meta(kv, P.mt, ws, &up)) return rc;
-  if (launch_layer(c, P, w, kv->layer_base(layer), x_in, x_out, (char*)ws, st, &up, aux))
+  if (launch_layer(c, P, w, kv, layer, x_in, x_out, (char*)ws, st, &up, aux))
     return fail(PS_E_UNSUPPORTED, "a kernel rejected its configuration");
   return last_launch_error();
 }
@@ -1659,7 +1721,7 @@ ps_status run_model(ps_model* M, ps_kv* kv, int32_t phase, int32_t n_chunk, cons
   char* cur = W + mw.xa;
   char* nxt = W + mw.xb;
   for (int l = 0; l < M->n_layers; ++l) {
-    bad |= launch_layer(c, P, &M->layers[l], kv->layer_base(l), cur, nxt, W, st);
+    bad |= launch_layer(c, P, &M->layers[l], kv, l, cur, nxt, W, st);
     std::swap(cur, nxt);
   }
   float* logits = logits_out ? logits_out : (float*)(W + mw.logits);
@@ -1907,9 +1969,13 @@ extern "C" ps_status ps_op_rope_kvwrite(ps_kv* kv, int32_t layer, int32_t n_seqs
   if (ps_status rc = kv->staging.submit(slot, ws, mt.buf.size(), st)) return rc;
   char* W = (char*)ws;
   const ps_layer_cfg& c = kv->cfg;
-  launch_rope_kvwrite(c.dtype, cs.rows, qkv, q_out, kv->layer_base(layer), (const SeqInfo*)(W + o_si),
-                      (const int32_t*)(W + o_bt), (const double*)(W + o_fr), n_seqs, c.n_q_heads, c.n_kv_heads,
-                      c.head_dim, fills_pages(cs.si), st);
+  if (kv->e4m3)
+    launch_kv8_rope_write(cs.rows, qkv, q_out, kv->layer8(layer), (const SeqInfo*)(W + o_si), (const int32_t*)(W + o_bt),
+                          (const double*)(W + o_fr), n_seqs, c.n_q_heads, c.n_kv_heads, c.head_dim, st);
+  else
+    launch_rope_kvwrite(c.dtype, cs.rows, qkv, q_out, kv->layer_base(layer), (const SeqInfo*)(W + o_si),
+                        (const int32_t*)(W + o_bt), (const double*)(W + o_fr), n_seqs, c.n_q_heads, c.n_kv_heads,
+                        c.head_dim, fills_pages(cs.si), st);
   return last_launch_error();
   PS_CATCH
 }
@@ -1927,7 +1993,7 @@ extern "C" ps_status ps_op_attention(ps_kv* kv, int32_t layer, int32_t n_seqs, c
   Meta mt;
   const size_t o_si = mt.add(cs.si.data(), cs.si.size() * sizeof(SeqInfo));
   const size_t o_bt = mt.add(cs.bt.data(), cs.bt.size() * 4);
-  const bool fa = fa_ok(c);
+  const bool fa = kv->e4m3 || fa_ok(c);
   std::vector<PrefillItem> pitems;
   PrefillSplit sp;
   size_t o_pi = 0, o_mg = 0, off_po = 0, off_ml = 0;
@@ -1936,7 +2002,7 @@ extern "C" ps_status ps_op_attention(ps_kv* kv, int32_t layer, int32_t n_seqs, c
     const size_t part = fa_part_bytes(c.n_q_heads), ml = fa_part_ml_bytes(c.n_q_heads);
     const size_t fixed = mt.size() + 2 * align_up(sizeof(PrefillSplitItem) * 3 * compute_units(), 256) + 1024;
     if (ws_bytes > fixed)
-      sp = plan_prefill_split(cs.si, cs.si.size(), c.n_kv_heads * (group_of(c) / 4), c.n_q_heads,
+      sp = plan_prefill_split(cs.si, cs.si.size(), fa_groups(c), c.n_q_heads,
                               [&] { return (int)std::min<size_t>((ws_bytes - fixed) / (part + ml), 1 << 20); });
     if (!sp.items.empty()) {
       o_pi = mt.add(sp.items.data(), sp.items.size() * sizeof(PrefillSplitItem));
@@ -1960,12 +2026,23 @@ extern "C" ps_status ps_op_attention(ps_kv* kv, int32_t layer, int32_t n_seqs, c
   char* W = (char*)ws;
   const float scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)c.head_dim));
   int bad;
-  if (fa && !sp.items.empty())
-    bad = launch_fa_prefill_split(group_of(c), (int)sp.items.size(), (int)sp.merges.size(), c.n_kv_heads, q,
-                                  kv->layer_base(layer), (const SeqInfo*)(W + o_si), (const int32_t*)(W + o_bt),
-                                  (const PrefillSplitItem*)(W + o_pi), (const PrefillMerge*)(W + o_mg),
-                                  FaPartials{{(float*)(W + off_po), nullptr, nullptr}, {sp.n_parts, sp.n_parts}, (float*)(W + off_ml)}, o,
-                                  scale_log2, st);
+  if (fa && !sp.items.empty()) {
+    const FaPartials parts{{(float*)(W + off_po), nullptr, nullptr}, {sp.n_parts, sp.n_parts}, (float*)(W + off_ml)};
+    const SeqInfo* si = (const SeqInfo*)(W + o_si);
+    const int32_t* bt = (const int32_t*)(W + o_bt);
+    const PrefillSplitItem* items = (const PrefillSplitItem*)(W + o_pi);
+    const PrefillMerge* merges = (const PrefillMerge*)(W + o_mg);
+    const int n_items = (int)sp.items.size(), n_merges = (int)sp.merges.size();
+    if (kv->e4m3)
+      bad = launch_kv8_prefill_split(group_of(c), c.head_dim, n_items, n_merges, c.n_kv_heads, q, kv->layer8(layer), si, bt,
+                                     items, merges, parts, o, scale_log2, st);
+    else
+      bad = launch_fa_prefill_split(group_of(c), n_items, n_merges, c.n_kv_heads, q, kv->layer_base(layer), si, bt, items,
+                                    merges, parts, o, scale_log2, st);
+  } else if (kv->e4m3)
+    bad = launch_kv8_prefill(group_of(c), c.head_dim, (int)pitems.size(), c.n_kv_heads, q, kv->layer8(layer),
+                             (const SeqInfo*)(W + o_si), (const int32_t*)(W + o_bt), (const PrefillItem*)(W + o_pi), o,
+                             scale_log2, st);
   else if (fa)
     bad = launch_fa_prefill(group_of(c), (int)pitems.size(), c.n_kv_heads, q, kv->layer_base(layer),
                             (const SeqInfo*)(W + o_si), (const int32_t*)(W + o_bt), (const PrefillItem*)(W + o_pi), o,
@@ -1984,7 +2061,7 @@ extern "C" ps_status ps_op_decode_plan(ps_kv* kv, int32_t n_seqs, const int32_t*
   PS_TRY CHECK_KV(kv);
   kv->dplan = DecodeAttnPlan{};
   const ps_layer_cfg& c = kv->cfg;
-  if (!dec_ok(c)) return fail(PS_E_UNSUPPORTED, "split-K decode attention needs bf16, head_dim 128, G <= 16");
+  if (!kv->e4m3 && !dec_ok(c)) return fail(PS_E_UNSUPPORTED, "split-K decode attention needs bf16, head_dim 128, G <= 16");
   if (split_pages < 0) return fail(PS_E_INVALID, "negative split_pages");
   CallSeqs cs;
   if (ps_status rc = plan_seqs(kv, n_seqs, seqs, nullptr, 1, cs)) return rc;
@@ -2036,11 +2113,18 @@ static ps_status decode_run(ps_kv* kv, int32_t layer, const void* q, void* o, vo
   const ps_layer_cfg& c = kv->cfg;
   char* W = (char*)ws;
   const float scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)c.head_dim));
-  int bad = launch_decode_attn(group_of(c), pl.n_items, c.n_kv_heads, pl.n_seqs, q, kv->layer_base(layer),
-                               (const SeqInfo*)(W + pl.o_si), (const int32_t*)(W + pl.o_bt),
-                               (const DecodeItem*)(W + pl.o_di), (float*)(W + pl.off_po), (float*)(W + pl.off_pml),
-                               (const int32_t*)(W + pl.o_pb), (const int32_t*)(W + pl.o_pc), o, scale_log2,
-                               (hipStream_t)stream, max_workgroups);
+  const SeqInfo* si = (const SeqInfo*)(W + pl.o_si);
+  const int32_t* bt = (const int32_t*)(W + pl.o_bt);
+  const DecodeItem* items = (const DecodeItem*)(W + pl.o_di);
+  float *po = (float*)(W + pl.off_po), *pml = (float*)(W + pl.off_pml);
+  const int32_t *pb = (const int32_t*)(W + pl.o_pb), *pc = (const int32_t*)(W + pl.o_pc);
+  int bad;
+  if (kv->e4m3)
+    bad = launch_kv8_decode(group_of(c), c.head_dim, pl.n_items, c.n_kv_heads, pl.n_seqs, q, kv->layer8(layer), si, bt, items,
+                            po, pml, pb, pc, o, scale_log2, (hipStream_t)stream, max_workgroups);
+  else
+    bad = launch_decode_attn(group_of(c), pl.n_items, c.n_kv_heads, pl.n_seqs, q, kv->layer_base(layer), si, bt, items, po,
+                             pml, pb, pc, o, scale_log2, (hipStream_t)stream, max_workgroups);
   if (bad) return fail(PS_E_UNSUPPORTED, "decode attention configuration not supported");
   return last_launch_error();
 }

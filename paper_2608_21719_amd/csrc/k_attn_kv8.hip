@@ -1,0 +1,584 @@
+// Attention over an e4m3 KV pool (gfx950): decode rows split over their keys,
+// and causal prefill or chunk rows. Layout and conversions: kv8.h.
+//
+// A byte times its page's power of two is exact in bf16, so both kernels widen
+// keys and values to bf16 operands (v_cvt_scalef32_pk_bf16_fp8: two values and
+// their scale in one instruction) and are from there the bf16 attention: bf16
+// MFMA with fp32 sums, fp32 softmax statistics, P rounded to bf16 for the second
+// product and the normaliser summing those rounded values. The query is not
+// rounded to 8 bits.
+#include "kv8.h"
+#include "launch.h"
+
+#include <type_traits>
+
+namespace ps {
+
+// ==================================================================== decode
+// A work item is (batch entry, logical page range); a workgroup does one KV head
+// of it, up to 16 query heads at a time (the rows of an MFMA tile; those past
+// the group are padding). Its four waves take pairs of pages w, w + 4, ... of the
+// range. Lane (g, c) of a wave has in its 16-byte chunks
+//   keys:   token c, dims 64 i + 16 g ..           two 16x16x32 MFMAs, with q's
+//                                                  columns read in that order
+//   values: tokens 4 g .. 4 g + 3 of dims 64 i + 16 b + c, b = 0 .. 3
+// and of the scores (S^T = K q^T) tokens 4 g + r of head c. P V therefore takes
+// both pages of a pair in one 16x16x32 MFMA per 16 dims, its 32 k slots being
+// (page, token) as the scores lie in the lane: k = 8 g + e is token 4 g + e % 4 of
+// page e / 4 for P and V alike, and nothing crosses lanes but the maximum.
+// The pass is bound by HBM: 16 loads of 1 KiB per pair and wave, all whole
+// lines, non-temporal, two pairs in flight behind the one at work.
+namespace {
+typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f4;
+}
+
+template <int HD>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void kv8_decode_kernel(
+    const bf16_t* __restrict__ q, Kv8Layer kv, const SeqInfo* __restrict__ si, const int32_t* __restrict__ bt,
+    const DecodeItem* __restrict__ items, float* __restrict__ part_o, float* __restrict__ part_ml, bf16_t* __restrict__ out,
+    int n_kv, int G, int n_items, float scale_log2) {
+  constexpr int NB = HD / 64;        // 64-dim blocks
+  const int kvh = blockIdx.x % n_kv, h0 = blockIdx.x / n_kv * 16;  // first query head within the group
+  const int nh = min(G - h0, 16);
+  const int n_q = n_kv * G;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  const int g = lane >> 4, c = lane & 15;
+  __shared__ float s_acc[4][16][HD];
+  __shared__ float s_m[4][16], s_l[4][16];
+  for (int iy = blockIdx.y; iy < n_items; iy += gridDim.y) {
+    const DecodeItem it = items[iy];
+    const SeqInfo s = si[it.b];
+    const int kv_len = s.kv_before + s.n_new;
+    const int32_t* btr = bt + s.bt_off;
+    bf16x8_t qb[NB][2];
+    {
+      const bf16_t* qp = q + ((long)it.b * n_q + kvh * G + h0 + min(c, nh - 1)) * HD + 16 * g;
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) qb[i][h] = __builtin_bit_cast(bf16x8_t, *(const uint4*)(qp + 64 * i + 8 * h));
+    }
+    float m = -INFINITY, l = 0.f;
+    f4 acc[4 * NB];
+#pragma unroll
+    for (int i = 0; i < 4 * NB; ++i) acc[i] = f4{0.f, 0.f, 0.f, 0.f};
+
+    struct Pair {
+      uint4 k[2][NB], v[2][NB];
+      float2 s[2];
+    };
+    const float2* scales = kv.scales + (long)kvh * kv.n_pages;
+    const int end = it.page_end;
+    auto load_page = [&](int p, uint4 (&k)[NB], uint4 (&v)[NB], float2& sc) __attribute__((always_inline)) {
+      const int page = btr[p];
+      const uint8_t* base = kv.blocks + kv8_block(page, kvh, n_kv, HD) + lane * 16;
+      sc = scales[page];
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
+        k[i] = __builtin_bit_cast(uint4, __builtin_nontemporal_load((const u32x4_t*)(base + 1024 * i)));
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
+        v[i] = __builtin_bit_cast(uint4, __builtin_nontemporal_load((const u32x4_t*)(base + kPageTokens * HD + 1024 * i)));
+    };
+    // pages p, p + 1; the second of an odd range's last pair is read as p again and masked
+    auto load = [&](int p, Pair& r) __attribute__((always_inline)) {
+      load_page(p, r.k[0], r.v[0], r.s[0]);
+      load_page(min(p + 1, end - 1), r.k[1], r.v[1], r.s[1]);
+    };
+    // `tail`: tokens at or past the sequence's end may be among the pair's
+    auto compute = [&](int p, Pair& r, auto tail) __attribute__((always_inline)) {
+      int valid[2] = {kPageTokens, kPageTokens};
+      if constexpr (decltype(tail)::value) {
+        valid[0] = kv_len - p * kPageTokens;
+        valid[1] = p + 1 < end ? kv_len - (p + 1) * kPageTokens : 0;
+      }
+      float sc[2][4], mx = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        f4 st = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+          st = __builtin_amdgcn_mfma_f32_16x16x32_bf16(e4m3_bf8(r.k[t][i].x, r.k[t][i].y, 1.f), qb[i][0], st, 0, 0, 0);
+          st = __builtin_amdgcn_mfma_f32_16x16x32_bf16(e4m3_bf8(r.k[t][i].z, r.k[t][i].w, 1.f), qb[i][1], st, 0, 0, 0);
+        }
+        const float f = scale_log2 * r.s[t].x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          sc[t][e] = st[e] * f;
+          if constexpr (decltype(tail)::value) sc[t][e] = 4 * g + e < valid[t] ? sc[t][e] : -INFINITY;
+          mx = fmaxf(mx, sc[t][e]);
+        }
+        if constexpr (decltype(tail)::value) {
+          // slots that hold no token yet may hold any byte: zero, so that 0 x NaN does not arise
+          const uint32_t keep = token_bytes(valid[t] - 4 * g);
+#pragma unroll
+          for (int i = 0; i < NB; ++i)
+            r.v[t][i] = make_uint4(r.v[t][i].x & keep, r.v[t][i].y & keep, r.v[t][i].z & keep, r.v[t][i].w & keep);
+        }
+      }
+      mx = fmaxf(mx, __shfl_xor(mx, 16));
+      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      const float m_new = fmaxf(m, mx);
+      const float base = m_new == -INFINITY ? 0.f : m_new;  // only scores of -inf yet: their weights are 0, not NaN
+      const float alpha = exp2f(m - base);
+      uint32_t pk[4];
+      float ps = 0.f;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          pk[2 * t + e] = pack_bf2(exp2f(sc[t][2 * e] - base), exp2f(sc[t][2 * e + 1] - base));
+          ps += bf_lo(pk[2 * t + e]) + bf_hi(pk[2 * t + e]);
+        }
+      l = l * alpha + ps;
+      m = m_new;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {  // acc rows are heads 4 g + e
+        const float a = __shfl(alpha, 4 * g + e);
+#pragma unroll
+        for (int i = 0; i < 4 * NB; ++i) acc[i][e] *= a;
+      }
+      const bf16x8_t pa = __builtin_bit_cast(bf16x8_t, make_uint4(pk[0], pk[1], pk[2], pk[3]));
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        const uint32_t v0[4] = {r.v[0][i].x, r.v[0][i].y, r.v[0][i].z, r.v[0][i].w};
+        const uint32_t v1[4] = {r.v[1][i].x, r.v[1][i].y, r.v[1][i].z, r.v[1][i].w};
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          const bf16x8_t vb = __builtin_bit_cast(
+              bf16x8_t, make_uint4(e4m3_bf2<false>(v0[b], r.s[0].y), e4m3_bf2<true>(v0[b], r.s[0].y),
+                                   e4m3_bf2<false>(v1[b], r.s[1].y), e4m3_bf2<true>(v1[b], r.s[1].y)));
+          acc[4 * i + b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa, vb, acc[4 * i + b], 0, 0, 0);
+        }
+      }
+    };
+    Pair r0, r1, r2;
+    int p = it.page_begin + 2 * wave;
+    constexpr int STEP = 8;
+    if (p < end) load(p, r0);
+    if (p + STEP < end) load(p + STEP, r1);
+    constexpr std::false_type kMid{};
+    constexpr std::true_type kTail{};
+    // the scheduling barriers keep requests ahead of the work before them
+    for (; p + 4 * STEP < end; p += 3 * STEP) {  // pairs p, p + STEP, p + 2 STEP are whole: p + 4 STEP exists
+      load(p + 2 * STEP, r2);
+      __builtin_amdgcn_sched_barrier(0);
+      compute(p, r0, kMid);
+      __builtin_amdgcn_sched_barrier(0);
+      load(p + 3 * STEP, r0);
+      __builtin_amdgcn_sched_barrier(0);
+      compute(p + STEP, r1, kMid);
+      __builtin_amdgcn_sched_barrier(0);
+      load(p + 4 * STEP, r1);
+      __builtin_amdgcn_sched_barrier(0);
+      compute(p + 2 * STEP, r2, kMid);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (p < end) {  // at most four pairs left
+      if (p + 2 * STEP < end) load(p + 2 * STEP, r2);
+      compute(p, r0, kTail);
+      if (p + STEP < end) {
+        if (p + 3 * STEP < end) load(p + 3 * STEP, r0);
+        compute(p + STEP, r1, kTail);
+        if (p + 2 * STEP < end) {
+          compute(p + 2 * STEP, r2, kTail);
+          if (p + 3 * STEP < end) compute(p + 3 * STEP, r0, kTail);
+        }
+      }
+    }
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    // merge the four waves
+    if (lane < 16) {
+      s_m[wave][lane] = m;
+      s_l[wave][lane] = l;
+    }
+#pragma unroll
+    for (int i = 0; i < 4 * NB; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s_acc[wave][4 * g + e][16 * i + c] = acc[i][e];
+    __syncthreads();
+    const bool whole = it.part < 0;  // a sequence in one split is finished here
+    const long part = (long)it.part * n_kv + kvh;
+    for (int e = threadIdx.x; e < nh * HD; e += 256) {
+      const int head = e / HD, dim = e - head * HD;
+      const float M = fmaxf(fmaxf(s_m[0][head], s_m[1][head]), fmaxf(s_m[2][head], s_m[3][head]));
+      float o = 0.f, L = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float f = s_m[w][head] == -INFINITY ? 0.f : exp2f(s_m[w][head] - M);
+        o += s_acc[w][head][dim] * f;
+        L += s_l[w][head] * f;
+      }
+      const int hg = h0 + head;
+      if (whole) {
+        out[((long)it.b * n_q + kvh * G + hg) * HD + dim] = f2bf(o / L);
+        continue;
+      }
+      part_o[(part * G + hg) * HD + dim] = o;
+      if (dim == 0) *(float2*)(part_ml + (part * G + hg) * 2) = make_float2(M, L);
+    }
+    __syncthreads();  // the next item reuses the LDS
+  }
+}
+
+// o = sum_s o_s 2^(m_s - M) / sum_s l_s 2^(m_s - M), splits in order.
+template <int HD>
+__global__ __launch_bounds__(HD) void kv8_combine_kernel(const float* __restrict__ part_o, const float* __restrict__ part_ml,
+                                                         const int32_t* __restrict__ part_begin,
+                                                         const int32_t* __restrict__ part_count, bf16_t* __restrict__ o,
+                                                         int n_q) {
+  const int b = blockIdx.x, head = blockIdx.y, dim = threadIdx.x;
+  const int np = part_count[b];
+  if (np == 1) return;  // written by the attention kernel
+  const long i0 = (long)part_begin[b] * n_q + head;  // part (p, head) is p n_q + head
+  float M = -INFINITY;
+  for (int i = 0; i < np; ++i) M = fmaxf(M, part_ml[(i0 + (long)i * n_q) * 2]);
+  float acc = 0.f, L = 0.f;
+  int i = 0;
+  for (; i + 4 <= np; i += 4) {  // four splits' loads overlap
+    float ov[4];
+    float2 ml[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const long pi = i0 + (long)(i + u) * n_q;
+      ov[u] = part_o[pi * HD + dim];
+      ml[u] = *(const float2*)(part_ml + pi * 2);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float f = ml[u].x == -INFINITY ? 0.f : exp2f(ml[u].x - M);
+      acc += ov[u] * f;
+      L += ml[u].y * f;
+    }
+  }
+  for (; i < np; ++i) {
+    const long pi = i0 + (long)i * n_q;
+    const float2 ml = *(const float2*)(part_ml + pi * 2);
+    const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
+    acc += part_o[pi * HD + dim] * f;
+    L += ml.y * f;
+  }
+  o[((long)b * n_q + head) * HD + dim] = f2bf(acc / L);
+}
+
+int launch_kv8_decode(int G, int hd, int n_items, int n_kv, int n_seqs, const void* q, const Kv8Layer& kv, const SeqInfo* si,
+                      const int32_t* bt, const DecodeItem* items, float* part_o, float* part_ml, const int32_t* part_begin,
+                      const int32_t* part_count, void* o, float scale_log2, hipStream_t st, int max_wg) {
+  if (n_seqs == 0) return 0;
+  if (n_items > kMaxDecodeItems) return -1;
+  const int gx = n_kv * ((G + 15) / 16);
+  const int gy = max_wg > 0 ? std::max(1, std::min(n_items, max_wg / gx)) : n_items;
+  auto go = [&](auto hc) {
+    constexpr int HD = decltype(hc)::value;
+    hipLaunchKernelGGL(kv8_decode_kernel<HD>, dim3(gx, gy), dim3(256), 0, st, (const bf16_t*)q, kv, si, bt, items, part_o,
+                       part_ml, (bf16_t*)o, n_kv, G, n_items, scale_log2);
+    if (n_items == n_seqs) return 0;  // every sequence in one split
+    hipLaunchKernelGGL(kv8_combine_kernel<HD>, dim3(n_seqs, n_kv * G), dim3(HD), 0, st, part_o, part_ml, part_begin,
+                       part_count, (bf16_t*)o, n_kv * G);
+    return 0;
+  };
+  if (hd == 128) return go(std::integral_constant<int, 128>{});
+  if (hd == 64) return go(std::integral_constant<int, 64>{});
+  return -1;
+}
+
+// =================================================================== prefill
+// A workgroup owns 32 query rows of one sequence and up to four query heads of
+// one KV head, a wave each (waves past the group repeat its last head and store
+// nothing), and walks 32-key tiles (two pages) up to its last row. As in the
+// bf16 kernel S^T = K Q^T and O^T = V^T P^T, so that a lane holds one query
+// column of both and the statistics never cross lanes but between its halves.
+//
+// A tile's bytes go through registers: waves 0, 2 widen the keys of its pages,
+// waves 1, 3 the values, once for all four heads (16 conversions and four to
+// eight LDS stores per lane and tile), while the tile before it is multiplied;
+// the bytes themselves were requested another tile earlier. Masking of slots
+// without a token rides on the conversion.
+// LDS, two slots: K row = key, 16-byte chunk p of row r holds dims of chunk p ^
+// (r % 16) (hd 64: of 8 chunks, r % 8). V^T per page: row = dim, 16 tokens with
+// the quads in the order 0 2 1 3, which is how P lies in a lane (k = 8 g + e: token
+// 4 g + e, or 8 + 4 g + e - 4), the 16-byte halves exchanged by bit 3 of the row.
+namespace {
+constexpr int kPT = 32;  // query rows per tile, keys per tile
+}
+
+// Workgroup barrier for LDS alone: a full fence would wait for the bytes in flight.
+__device__ __forceinline__ void kv8_lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+template <int HD, bool SPLIT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void kv8_prefill_kernel(
+    const bf16_t* __restrict__ q, Kv8Layer kv, const SeqInfo* __restrict__ si, const int32_t* __restrict__ bt,
+    const typename std::conditional<SPLIT, PrefillSplitItem, PrefillItem>::type* __restrict__ items, bf16_t* __restrict__ o,
+    int n_kv, int G, float scale_log2, FaPartials parts) {
+  constexpr int KT = kPT, KK = HD / 16, DB = HD / 32, NB = HD / 64, CH = HD / 8;  // CH: 16-byte chunks of a K row
+  constexpr int KE = kPageTokens * HD;  // elements of a page's keys
+  __shared__ __attribute__((aligned(1024))) bf16_t sK[2][KT * HD];
+  __shared__ __attribute__((aligned(1024))) bf16_t sV[2][KT * HD];
+  const int hq = (G + 3) / 4;
+  const int kvh = blockIdx.y / hq;
+  const auto it = items[blockIdx.x];
+  const SeqInfo s = si[it.b];
+  const int n_q = n_kv * G;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int g = lane >> 5, c = lane & 31;
+  const int hi = (blockIdx.y % hq) * 4 + wave;
+  const bool live = hi < G;
+  const int head = kvh * G + min(hi, G - 1);
+  const int qn = min(kPT, s.n_new - it.q_begin);
+  const int qpos0 = s.kv_before + it.q_begin;
+  const int kv_valid = s.kv_before + s.n_new;
+  const int32_t* btr = bt + s.bt_off;
+  int kt0 = 0, n_tiles = (qpos0 + qn + KT - 1) / KT;
+  if constexpr (SPLIT) kt0 = it.kt_begin, n_tiles = it.kt_end;
+  const float2* scales = kv.scales + (long)kvh * kv.n_pages;
+
+  // this wave's half of one page of a tile
+  const int pg = wave >> 1;
+  const bool values = wave & 1;
+  struct Raw {
+    uint4 w[NB];
+    float s;
+    int valid;  // tokens of the page that are written
+  };
+  auto fetch = [&](int kt) __attribute__((always_inline)) {
+    Raw r;
+    const int p = 2 * kt + pg;
+    r.valid = kv_valid - p * kPageTokens;
+    r.s = 0.f;
+#pragma unroll
+    for (int i = 0; i < NB; ++i) r.w[i] = make_uint4(0, 0, 0, 0);
+    if (r.valid > 0) {
+      const int page = btr[p];
+      const uint8_t* base = kv.blocks + kv8_block(page, kvh, n_kv, HD) + (values ? KE : 0) + lane * 16;
+      const float2 sc = scales[page];
+      r.s = values ? sc.y : sc.x;
+#pragma unroll
+      for (int i = 0; i < NB; ++i) r.w[i] = *(const uint4*)(base + 1024 * i);
+    }
+    return r;
+  };
+  const int lq = lane >> 4, lc = lane & 15;
+  auto put = [&](const Raw& r, int slot) __attribute__((always_inline)) {
+    if (!values) {  // lane: token lc, dims 64 i + 16 lq ..
+      char* row = (char*)sK[slot] + (16 * pg + lc) * HD * 2;
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        const int ch = 8 * i + 2 * lq;
+        *(bf16x8_t*)(row + ((ch ^ (lc & (CH - 1))) << 4)) = e4m3_bf8(r.w[i].x, r.w[i].y, r.s);
+        *(bf16x8_t*)(row + (((ch + 1) ^ (lc & (CH - 1))) << 4)) = e4m3_bf8(r.w[i].z, r.w[i].w, r.s);
+      }
+    } else {  // lane: tokens 4 lq .., dims 64 i + 16 b + lc
+      const uint32_t keep = token_bytes(r.valid - 4 * lq);
+      char* page = (char*)sV[slot] + pg * KE * 2;
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        const uint32_t w[4] = {r.w[i].x, r.w[i].y, r.w[i].z, r.w[i].w};
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          const int dim = 64 * i + 16 * b + lc;
+          const uint32_t x = w[b] & keep;
+          *(uint2*)(page + dim * 32 + (((lq & 1) ^ ((dim >> 3) & 1)) << 4) + ((lq >> 1) << 3)) =
+              make_uint2(e4m3_bf2<false>(x, r.s), e4m3_bf2<true>(x, r.s));
+        }
+      }
+    }
+  };
+
+  bf16x8_t qf[KK];
+  {
+    const bf16_t* qp = q + ((long)(s.row_start + it.q_begin + min(c, qn - 1)) * n_q + head) * HD + 8 * g;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) qf[kk] = __builtin_bit_cast(bf16x8_t, *(const uint4*)(qp + 16 * kk));
+  }
+  f32x16_t oacc[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) oacc[db][r] = 0.f;
+  float lsum = 0.f, m = -INFINITY, mb = -INFINITY;  // row max behind the exponent base, and m scale
+  typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+  const bf16x2_t ones2 = {(__bf16)1.0f, (__bf16)1.0f};
+  const uint32_t kread = (uint32_t)(c * HD * 2 + ((g ^ (c & (CH - 1))) << 4));
+  const uint32_t vread = (uint32_t)(c * 32 + ((g ^ ((c >> 3) & 1)) << 4));
+  const int qpos = qpos0 + min(c, qn - 1);  // padding columns take the last row's keys
+
+  Raw next = fetch(kt0);
+  put(next, 0);
+  if (kt0 + 1 < n_tiles) next = fetch(kt0 + 1);
+  kv8_lds_barrier();
+
+  auto tile = [&](int kt, int slot, auto firstc) __attribute__((always_inline)) {
+    constexpr bool FIRST = decltype(firstc)::value;
+    const int k0 = kt * KT;
+    const char *K = (const char*)sK[slot], *V = (const char*)sV[slot];
+    if (kt + 1 < n_tiles) {
+      put(next, slot ^ 1);
+      if (kt + 2 < n_tiles) next = fetch(kt + 2);
+    }
+    f32x16_t sacc;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sacc[r] = 0.f;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      const bf16x8_t a = __builtin_bit_cast(bf16x8_t, *(const uint4*)(K + (kread ^ (32 * kk))));
+      sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[kk], sacc, 0, 0, 0);
+    }
+    if (k0 + KT - 1 > qpos0) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (k0 + 8 * (r >> 2) + 4 * g + (r & 3) > qpos) sacc[r] = -INFINITY;
+    }
+    // P = 2^(s scale - mb). The exponent base is not the running maximum: the
+    // first tile sets it from its own, after that the sum of the tile's P, taken
+    // anyway, shows where it no longer fits (past 2^32, infinite or NaN), and
+    // only then is the true maximum taken, O and l rescaled and P redone.
+    uint32_t pk[8];
+    auto exps = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        pk[i] = pack_bf2(__builtin_amdgcn_exp2f(fmaf(sacc[2 * i], scale_log2, -mb)),
+                         __builtin_amdgcn_exp2f(fmaf(sacc[2 * i + 1], scale_log2, -mb)));
+      float lt = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) lt = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, pk[i]), ones2, lt, false);
+      return lt;
+    };
+    auto row_max = [&]() __attribute__((always_inline)) {
+      float mx = sacc[0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sacc[r]);
+      const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+      return fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+    };
+    // while every score so far is -inf the base stays -inf, which sends the next tile here too
+    float lt;
+    if constexpr (FIRST) {
+      m = row_max();
+      const bool none = m == -INFINITY;
+      mb = none ? 0.f : m * scale_log2;
+      lt = exps();
+      if (none) mb = -INFINITY;
+    } else {
+      lt = exps();
+      if (__any(!(lt <= 0x1p32f))) {
+        const float m_new = fmaxf(m, row_max());
+        const bool none = m_new == -INFINITY;
+        const float alpha = none ? 1.f : __builtin_amdgcn_exp2f((m - m_new) * scale_log2);
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) oacc[db][r] *= alpha;
+        lsum *= alpha;
+        m = m_new;
+        mb = none ? 0.f : m * scale_log2;
+        lt = exps();
+        if (none) mb = -INFINITY;
+      }
+    }
+    lsum += lt;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const bf16x8_t bp = __builtin_bit_cast(bf16x8_t, make_uint4(pk[4 * p], pk[4 * p + 1], pk[4 * p + 2], pk[4 * p + 3]));
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const bf16x8_t a = __builtin_bit_cast(bf16x8_t, *(const uint4*)(V + p * KE * 2 + db * 32 * 32 + vread));
+        oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, bp, oacc[db], 0, 0, 0);
+      }
+    }
+    kv8_lds_barrier();  // the next tile is written; every wave is done with this one
+  };
+  tile(kt0, 0, std::true_type{});
+  for (int kt = kt0 + 1; kt < n_tiles; ++kt) tile(kt, (kt - kt0) & 1, std::false_type{});
+
+  const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(lsum), __float_as_uint(lsum), false, false);
+  const float l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+  if (!live || c >= qn) return;
+  if constexpr (SPLIT) {
+    if (it.part >= 0) {
+      float* po = parts.part(it.part, (long)n_q * kPT * HD) + ((long)head * kPT + c) * HD;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int rb = 0; rb < 4; ++rb)
+          *(float4*)(po + 32 * db + 8 * rb + 4 * g) =
+              make_float4(oacc[db][4 * rb], oacc[db][4 * rb + 1], oacc[db][4 * rb + 2], oacc[db][4 * rb + 3]);
+      if (g == 0) *(float2*)(parts.ml + (((long)it.part * n_q + head) * kPT + c) * 2) = make_float2(mb, l);
+      return;
+    }
+  }
+  const float inv = 1.f / l;
+  bf16_t* op = o + ((long)(s.row_start + it.q_begin + c) * n_q + head) * HD;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int rb = 0; rb < 4; ++rb)
+      *(uint2*)(op + 32 * db + 8 * rb + 4 * g) =
+          make_uint2(pack_bf2(oacc[db][4 * rb] * inv, oacc[db][4 * rb + 1] * inv),
+                     pack_bf2(oacc[db][4 * rb + 2] * inv, oacc[db][4 * rb + 3] * inv));
+}
+
+// Parts of a split query tile, in key order; a wave per head and row.
+template <int HD>
+__global__ __launch_bounds__(256) void kv8_merge_kernel(const PrefillMerge* __restrict__ merges, FaPartials parts,
+                                                        bf16_t* __restrict__ o, int n_q) {
+  constexpr int W = HD / 64;  // dims per lane
+  const PrefillMerge mg = merges[blockIdx.x / kPT];
+  const int c = blockIdx.x % kPT;
+  const int head = blockIdx.y * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (c >= mg.n_rows || head >= n_q) return;
+  const float* ml = parts.ml + (((long)mg.part * n_q + head) * kPT + c) * 2;
+  const long step = (long)n_q * kPT * 2;
+  float M = -INFINITY;
+  for (int p = 0; p < mg.n_parts; ++p) M = fmaxf(M, ml[p * step]);
+  float x[W] = {}, L = 0.f;
+  for (int p = 0; p < mg.n_parts; ++p) {
+    const float* po = parts.part(mg.part + p, (long)n_q * kPT * HD) + ((long)head * kPT + c) * HD + W * lane;
+    const float f = ml[p * step] == -INFINITY ? 0.f : exp2f(ml[p * step] - M);
+#pragma unroll
+    for (int i = 0; i < W; ++i) x[i] += po[i] * f;
+    L += ml[p * step + 1] * f;
+  }
+  bf16_t* op = o + ((long)(mg.row + c) * n_q + head) * HD + W * lane;
+#pragma unroll
+  for (int i = 0; i < W; ++i) op[i] = f2bf(x[i] / L);
+}
+
+int launch_kv8_prefill(int G, int hd, int n_items, int n_kv, const void* q, const Kv8Layer& kv, const SeqInfo* si,
+                       const int32_t* bt, const PrefillItem* items, void* o, float scale_log2, hipStream_t st) {
+  if (n_items == 0) return 0;
+  auto go = [&](auto hc) {
+    hipLaunchKernelGGL((kv8_prefill_kernel<decltype(hc)::value, false>), dim3(n_items, n_kv * ((G + 3) / 4)), dim3(256), 0, st,
+                       (const bf16_t*)q, kv, si, bt, items, (bf16_t*)o, n_kv, G, scale_log2, FaPartials{});
+    return 0;
+  };
+  if (hd == 128) return go(std::integral_constant<int, 128>{});
+  if (hd == 64) return go(std::integral_constant<int, 64>{});
+  return -1;
+}
+
+int launch_kv8_prefill_split(int G, int hd, int n_items, int n_merges, int n_kv, const void* q, const Kv8Layer& kv,
+                             const SeqInfo* si, const int32_t* bt, const PrefillSplitItem* items, const PrefillMerge* merges,
+                             FaPartials part, void* o, float scale_log2, hipStream_t st) {
+  if (n_items == 0) return 0;
+  const int n_q = n_kv * G;
+  auto go = [&](auto hc) {
+    constexpr int HD = decltype(hc)::value;
+    hipLaunchKernelGGL((kv8_prefill_kernel<HD, true>), dim3(n_items, n_kv * ((G + 3) / 4)), dim3(256), 0, st,
+                       (const bf16_t*)q, kv, si, bt, items, (bf16_t*)o, n_kv, G, scale_log2, part);
+    if (n_merges > 0)
+      hipLaunchKernelGGL(kv8_merge_kernel<HD>, dim3(n_merges * kPT, (n_q + 3) / 4), dim3(256), 0, st, merges, part, (bf16_t*)o,
+                         n_q);
+    return 0;
+  };
+  if (hd == 128) return go(std::integral_constant<int, 128>{});
+  if (hd == 64) return go(std::integral_constant<int, 64>{});
+  return -1;
+}
+
+}  // namespace ps

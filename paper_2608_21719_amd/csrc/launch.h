@@ -8,6 +8,7 @@
 #include <vector>
 
 #include "common.h"
+#include "kv8.h"
 
 namespace ps {
 
@@ -90,6 +91,31 @@ int launch_fa_prefill_split(int G, int n_items, int n_merges, int n_kv, const vo
                             const PrefillMerge* merges, FaPartials part, void* o, float scale_log2, hipStream_t st);
 int launch_fa_prefill(int G, int n_items, int n_kv, const void* q, const void* pool_layer, const SeqInfo* si,
                       const int32_t* bt, const PrefillItem* items, void* o, float scale_log2, hipStream_t st);
+
+// ------------------------------------------------------------ e4m3 KV pools
+// RoPE + KV write into an e4m3 pool (bf16 rows, head_dim 64 or 128); part and
+// splits as launch_rope_kvwrite.
+int launch_kv8_rope_write(int rows, const void* qkv, void* q_out, const Kv8Layer& kv, const SeqInfo* si, const int32_t* bt,
+                          const double* inv_freq, int n_seqs, int n_q, int n_kv, int hd, hipStream_t st,
+                          const float* part = nullptr, int splits = 1);
+int launch_kv8_append(int rows, const void* k, const void* v, const Kv8Layer& kv, const SeqInfo* si, const int32_t* bt,
+                      int n_seqs, int n_kv, int hd, hipStream_t st);
+int launch_kv8_gather(int len, const Kv8Layer& kv, const int32_t* bt, void* k_out, void* v_out, int n_kv, int hd,
+                      hipStream_t st);
+// Scales of one sequence's n_pages pages, `rows` = layers x KV heads.
+int launch_kv8_copy_scales(const float2* src, int src_pages, const int32_t* src_bt, float2* dst, int dst_pages,
+                           const int32_t* dst_bt, int n_pages, int rows, hipStream_t st);
+// Decode rows, any group size; work list and partials as launch_decode_attn.
+int launch_kv8_decode(int G, int hd, int n_items, int n_kv, int n_seqs, const void* q, const Kv8Layer& kv, const SeqInfo* si,
+                      const int32_t* bt, const DecodeItem* items, float* part_o, float* part_ml, const int32_t* part_begin,
+                      const int32_t* part_count, void* o, float scale_log2, hipStream_t st, int max_wg = 0);
+// Prefill rows, any group size; work lists and partials as launch_fa_prefill and
+// launch_fa_prefill_split (the same query and key tiles).
+int launch_kv8_prefill(int G, int hd, int n_items, int n_kv, const void* q, const Kv8Layer& kv, const SeqInfo* si,
+                       const int32_t* bt, const PrefillItem* items, void* o, float scale_log2, hipStream_t st);
+int launch_kv8_prefill_split(int G, int hd, int n_items, int n_merges, int n_kv, const void* q, const Kv8Layer& kv,
+                             const SeqInfo* si, const int32_t* bt, const PrefillSplitItem* items, const PrefillMerge* merges,
+                             FaPartials part, void* o, float scale_log2, hipStream_t st);
 
 // GEMM C = epi(A W^T); ws holds split-K partials for decode-sized M.
 // beside: another stream's kernels hold part of the chip, so a tile launch is
