@@ -509,6 +509,47 @@ ps_status ps_op_gemm_static(int32_t dtype, int32_t r_dtype, int32_t c_dtype, int
                             int32_t N, int32_t K, const void* A, const void* W, const void* R, void* C,
                             void* stream);
 
+/* ------------------------------------------------ products in 8-bit integers
+ * A linear layer as y = x W^T with x and W rounded to int8: one scale for each
+ * row of x (token) and each row of W (output channel). Decode reads half the
+ * weight bytes of bf16, prefill runs at twice the matrix rate (§III-B's roofline
+ * terms both ways). */
+
+/* q[r, :] = x[r, :] 127 / max|x[r, :]| rounded to the nearest integer (ties to
+ * even), scale[r] = max|x[r, :]| / 127, so that q scale stands for x. x [rows, d]
+ * of x_dtype (PS_F32 or PS_BF16), q int8 [rows, d], scale fp32 [rows]. A row with
+ * an infinity or NaN gets q = 0 and scale = NaN (its products are NaN, no other
+ * row's); a row below 2^-100 throughout q = 0 and scale 0. Also how a weight
+ * [N, K] gets its int8 values and channel scales. */
+ps_status ps_op_quant_rows(int32_t x_dtype, int32_t rows, int32_t d, const void* x, void* q, float* scale, void* stream);
+
+/* The same of the rows' RMSNorm, x / sqrt(mean(x^2) + eps) * g in fp32, which is
+ * not rounded in between. g [d] of g_dtype. */
+ps_status ps_op_rmsnorm_quant(int32_t x_dtype, int32_t g_dtype, int32_t rows, int32_t d, const void* x, const void* g,
+                              float eps, void* q, float* scale, void* stream);
+
+/* int8 weights are stored in tiles of 64 x 128, padded with zeros: W[n, k] is at
+ *   ((n / 64) * ceil(in / 128) + k / 128) * 8192 + (n % 64) * 128 + k % 128.
+ * ps_tiled_weight_i8_bytes: bytes of the tiled form (0 for sizes refused).
+ * ps_tile_weight_i8 (host) and ps_op_tile_weight_i8 (device, enqueued on stream)
+ * convert a row-major int8 [N, K]; K a multiple of 64 (else PS_E_UNSUPPORTED). */
+size_t ps_tiled_weight_i8_bytes(int32_t N, int32_t K);
+ps_status ps_tile_weight_i8(const void* w, int32_t N, int32_t K, void* out);
+ps_status ps_op_tile_weight_i8(int32_t N, int32_t K, const void* w, void* out, void* stream);
+
+/* C[m, n] = epilogue(a_scale[m] w_scale[n] sum_k A[m, k] W[n, k]): A int8 [M, K]
+ * row-major, W int8 [N, K] in the tiles above, a_scale fp32 [M], w_scale fp32 [N];
+ * the sum is exact in int32, everything after it fp32. Epilogues, R and C as
+ * ps_op_gemm (SwiGLU: W rows and w_scale in w_gate_up's order; r_dtype is read
+ * for PS_EPI_RESIDUAL only). c_dtype PS_F32 or PS_BF16; R of r_dtype may alias C
+ * when the dtypes match. N and K multiples of 64, K < 131072 (the sums then fit),
+ * any M; M <= 64 needs ws of ps_op_gemm_i8_workspace_bytes (0 bytes otherwise). The
+ * result does not depend on how the product is cut up: calls repeat bit for bit. */
+size_t ps_op_gemm_i8_workspace_bytes(int32_t M, int32_t N, int32_t K);
+ps_status ps_op_gemm_i8(int32_t r_dtype, int32_t c_dtype, int32_t epilogue, int32_t M, int32_t N, int32_t K, const void* A,
+                        const float* a_scale, const void* W, const float* w_scale, const void* R, void* C, void* ws,
+                        size_t ws_bytes, void* stream);
+
 /* RoPE + paged KV write for `layer`: qkv [rows, d_q + 2 d_kv] (cfg.dtype)
  * holds the QKV projection of rows grouped by sequence as in ps_prefill;
  * writes rotated q to q_out [rows, d_q] and rotated k and v into the pages

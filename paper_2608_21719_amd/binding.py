@@ -141,6 +141,13 @@ _SIGS = {
     "ps_op_gemm_workspace_bytes": (c_size_t, [_I, _I, _I, _I]),
     "ps_op_gemm": (_I, [_I, _I, _I, _I, _I, _I, _I, _P, _P, _P, _P, _P, c_size_t, _P]),
     "ps_op_gemm_static": (_I, [_I, _I, _I, _I, _I, _I, _I, _P, _P, _P, _P, _P]),
+    "ps_op_quant_rows": (_I, [_I, _I, _I, _P, _P, _P, _P]),
+    "ps_op_rmsnorm_quant": (_I, [_I, _I, _I, _I, _P, _P, c_float, _P, _P, _P]),
+    "ps_tiled_weight_i8_bytes": (c_size_t, [_I, _I]),
+    "ps_tile_weight_i8": (_I, [_P, _I, _I, _P]),
+    "ps_op_tile_weight_i8": (_I, [_I, _I, _P, _P, _P]),
+    "ps_op_gemm_i8_workspace_bytes": (c_size_t, [_I, _I, _I]),
+    "ps_op_gemm_i8": (_I, [_I, _I, _I, _I, _I, _I, _P, _P, _P, _P, _P, _P, _P, c_size_t, _P]),
     "ps_op_rope_kvwrite": (_I, [_P, _I, _I, _IP, _IP, _P, _P, _P, c_size_t, _P]),
     "ps_op_gemm_static": (_I, [_I, _I, _I, _I, _I, _I, _I, _P, _P, _P, _P, _P]),
     "ps_op_attention": (_I, [_P, _I, _I, _IP, _IP, _P, _P, _P, c_size_t, _P]),
@@ -239,6 +246,25 @@ def tile_weight(w):
 def op_tile_weight(dtype, N, K, w, out, stream=None):
     """Device conversion of a row-major [N, K] weight to the tiled layout."""
     check(lib.ps_op_tile_weight(dtype, N, K, ptr(w), ptr(out), stream_handle(stream)))
+
+
+def tiled_weight_i8_bytes(N: int, K: int) -> int:
+    return lib.ps_tiled_weight_i8_bytes(N, K)
+
+
+def tile_weight_i8(w):
+    """Host numpy conversion of a row-major int8 [N, K] weight to its tiled layout (a flat int8 array)."""
+    import numpy as np
+    w = np.ascontiguousarray(w, dtype=np.int8)
+    N, K = w.shape
+    out = np.empty(tiled_weight_i8_bytes(N, K), dtype=np.int8)
+    check(lib.ps_tile_weight_i8(ptr(w), N, K, ptr(out)))
+    return out
+
+
+def op_tile_weight_i8(N, K, w, out, stream=None):
+    """Device conversion of a row-major int8 [N, K] weight to its tiled layout."""
+    check(lib.ps_op_tile_weight_i8(N, K, ptr(w), ptr(out), stream_handle(stream)))
 
 
 # ---------------------------------------------------------------- handles
@@ -551,6 +577,24 @@ def op_gemm_static(dtype, r_dt, c_dt, epi, M, N, K, A, W, R, C, stream=None):
     """ps_op_gemm with split-K partials in the library's static device array (no workspace)."""
     check(lib.ps_op_gemm_static(dtype, r_dt, c_dt, epi, M, N, K, ptr(A), ptr(W), ptr(R), ptr(C),
                                 stream_handle(stream)))
+
+
+def op_quant_rows(x_dt, rows, d, x, q, scale, stream=None):
+    check(lib.ps_op_quant_rows(x_dt, rows, d, ptr(x), ptr(q), ptr(scale), stream_handle(stream)))
+
+
+def op_rmsnorm_quant(x_dt, g_dt, rows, d, x, g, eps, q, scale, stream=None):
+    check(lib.ps_op_rmsnorm_quant(x_dt, g_dt, rows, d, ptr(x), ptr(g), eps, ptr(q), ptr(scale), stream_handle(stream)))
+
+
+def op_gemm_i8_workspace_bytes(M, N, K) -> int:
+    return lib.ps_op_gemm_i8_workspace_bytes(M, N, K)
+
+
+def op_gemm_i8(r_dt, c_dt, epi, M, N, K, A, a_scale, W, w_scale, R, C, ws=None, stream=None):
+    wsb = 0 if ws is None else ws.numel() * ws.element_size()
+    check(lib.ps_op_gemm_i8(r_dt, c_dt, epi, M, N, K, ptr(A), ptr(a_scale), ptr(W), ptr(w_scale), ptr(R), ptr(C), ptr(ws),
+                            wsb, stream_handle(stream)))
 
 
 def op_rope_kvwrite(kv: KV, layer, seqs, n_tok, qkv, q_out, ws, stream=None):

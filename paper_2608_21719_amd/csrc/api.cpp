@@ -1945,6 +1945,77 @@ extern "C" ps_status ps_op_tile_weight(int32_t dtype, int32_t N, int32_t K, cons
   PS_CATCH
 }
 
+extern "C" size_t ps_tiled_weight_i8_bytes(int32_t N, int32_t K) {
+  if (N <= 0 || K <= 0 || K % 64) return 0;
+  return (size_t)tiled_weight_elems(N, K / 2) * 2;
+}
+
+// A 64 x 128 int8 tile is a 64 x 64 tile of pairs.
+extern "C" ps_status ps_tile_weight_i8(const void* w, int32_t N, int32_t K, void* out) {
+  PS_TRY
+  if (N > 0 && K > 0 && K % 64) return fail(PS_E_UNSUPPORTED, "K must be a multiple of 64");
+  return ps_tile_weight(w, N, K / 2, 2, out);
+  PS_CATCH
+}
+
+extern "C" ps_status ps_op_tile_weight_i8(int32_t N, int32_t K, const void* w, void* out, void* stream) {
+  PS_TRY
+  if (!w || !out || N <= 0 || K <= 0) return fail(PS_E_INVALID, "bad arguments");
+  if (K % 64) return fail(PS_E_UNSUPPORTED, "K must be a multiple of 64");
+  if (ps_status rc = check_aligned({w, out})) return rc;
+  if (launch_tile_weight(2, N, K / 2, w, out, (hipStream_t)stream)) return fail(PS_E_UNSUPPORTED, "element size");
+  return last_launch_error();
+  PS_CATCH
+}
+
+static ps_status quant_rows(int32_t x_dt, int32_t g_dt, int32_t rows, int32_t d, const void* x, const void* g, bool norm,
+                            float eps, void* q, float* scale, void* stream) {
+  if (rows < 0 || d <= 0) return fail(PS_E_INVALID, "bad shape");
+  if (rows > 0 && (!x || !q || !scale || (norm && !g))) return fail(PS_E_INVALID, "null pointer");
+  if (ps_status rc = check_aligned({x, g, q, scale})) return rc;
+  for (int dt : {x_dt, g_dt})
+    if (dt != PS_F32 && dt != PS_BF16) return fail(PS_E_INVALID, "bad dtype");
+  if (norm && !(eps >= 0.f)) return fail(PS_E_INVALID, "bad eps");
+  if (rows == 0) return PS_OK;
+  if (launch_quant_rows(x_dt, g_dt, rows, d, x, norm ? g : nullptr, eps, q, scale, (hipStream_t)stream))
+    return fail(PS_E_UNSUPPORTED, "dtype combination not supported");
+  return last_launch_error();
+}
+
+extern "C" ps_status ps_op_quant_rows(int32_t x_dt, int32_t rows, int32_t d, const void* x, void* q, float* scale,
+                                      void* stream) {
+  PS_TRY return quant_rows(x_dt, PS_F32, rows, d, x, nullptr, false, 0.f, q, scale, stream);
+  PS_CATCH
+}
+
+extern "C" ps_status ps_op_rmsnorm_quant(int32_t x_dt, int32_t g_dt, int32_t rows, int32_t d, const void* x, const void* g,
+                                         float eps, void* q, float* scale, void* stream) {
+  PS_TRY return quant_rows(x_dt, g_dt, rows, d, x, g, true, eps, q, scale, stream);
+  PS_CATCH
+}
+
+extern "C" size_t ps_op_gemm_i8_workspace_bytes(int32_t M, int32_t N, int32_t K) {
+  return gemm_i8_workspace_bytes(M, N, K);
+}
+
+extern "C" ps_status ps_op_gemm_i8(int32_t r_dt, int32_t c_dt, int32_t epi, int32_t M, int32_t N, int32_t K, const void* A,
+                                   const float* a_scale, const void* Wt, const float* w_scale, const void* R, void* C,
+                                   void* ws, size_t ws_bytes, void* stream) {
+  PS_TRY
+  if (epi < 0 || epi > 2) return fail(PS_E_INVALID, "bad epilogue");
+  if (M < 0 || N <= 0 || K <= 0) return fail(PS_E_INVALID, "bad shape");
+  if (M > 0 && (!A || !a_scale || !Wt || !w_scale || !C || (epi == 1 && !R))) return fail(PS_E_INVALID, "null pointer");
+  if (ps_status rc = check_aligned({A, a_scale, Wt, w_scale, R, C, ws})) return rc;
+  if (gemm_i8_check(epi, M, N, K)) return fail(PS_E_UNSUPPORTED, "int8 GEMM: N and K multiples of 64, K below 131072");
+  const size_t need = gemm_i8_workspace_bytes(M, N, K);
+  if (need && (!ws || ws_bytes < need)) return fail(PS_E_INVALID, "workspace too small for split-K partials");
+  if (M == 0) return PS_OK;
+  if (launch_gemm_i8(r_dt, c_dt, epi, M, N, K, A, a_scale, Wt, w_scale, R, C, ws, ws_bytes, (hipStream_t)stream))
+    return fail(PS_E_UNSUPPORTED, "dtype/epilogue combination not supported");
+  return last_launch_error();
+  PS_CATCH
+}
+
 extern "C" ps_status ps_op_rope_kvwrite(ps_kv* kv, int32_t layer, int32_t n_seqs, const int32_t* seqs,
                                         const int32_t* n_tok, const void* qkv, void* q_out, void* ws,
                                         size_t ws_bytes, void* stream) {

@@ -78,6 +78,48 @@ __device__ __forceinline__ void lds_barrier_pinned() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
+// The two operand types of the tile and the skinny GEMM. Both move 16-bit units:
+// bf16 values, or pairs of int8 values, so a GEMM of int8 operands and K has the
+// loads, the LDS layout and the schedule of a bf16 one of K / 2, and its MFMA takes
+// the same 16 bytes per lane (twice the k) in the same time.
+// Scales of the int32 sums.
+struct NoScales {};
+struct I8Scales {
+  const float* row;  // [M], of A's rows
+  const float* col;  // [N], of W's
+};
+template <typename TE> struct Operand;
+template <> struct Operand<bf16_t> {
+  static constexpr bool kInt8 = false;
+  using Frag = bf16x8_t;
+  using Acc16 = f32x16_t;  // 32x32 output
+  using Acc4 = f32x4_t;    // 16x16 output
+  using Sum = float;
+  using Scales = NoScales;
+  __device__ static __forceinline__ Acc16 mfma32(Frag a, Frag b, Acc16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
+  __device__ static __forceinline__ Acc4 mfma16(Frag a, Frag b, Acc4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+  }
+};
+typedef int i32x4_t __attribute__((ext_vector_type(4)));
+typedef int i32x16_t __attribute__((ext_vector_type(16)));
+template <> struct Operand<int8_t> {
+  static constexpr bool kInt8 = true;
+  using Frag = i32x4_t;
+  using Acc16 = i32x16_t;
+  using Acc4 = i32x4_t;
+  using Sum = int;
+  using Scales = I8Scales;
+  __device__ static __forceinline__ Acc16 mfma32(Frag a, Frag b, Acc16 c) {
+    return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0);
+  }
+  __device__ static __forceinline__ Acc4 mfma16(Frag a, Frag b, Acc4 c) {
+    return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
+  }
+};
+
 // f(std::integral_constant<int, i>) for i = B .. E-1, unrolled at compile
 // time (register arrays indexed by i stay in registers).
 template <int B, int E, typename F>
@@ -162,11 +204,18 @@ struct Geo {
 constexpr int share(int n, int mf, int q) { return n * q / mf; }
 }  // namespace tile
 
-template <int QM, int QN, int NS, bool NT, int EPI, typename TR, typename TC>
+// K in 16-bit units. int8 operands (Operand<int8_t>): N a multiple of 64 that
+// need not fill the last tile, K one of 32 units (W's tiles are padded with
+// zeros, whatever A's next row or the end of the buffer gives beside them).
+template <typename TE, int QM, int QN, int NS, bool NT, int EPI, typename TR, typename TC>
 __global__ __launch_bounds__(256) void gemm_tile_kernel(const bf16_t* __restrict__ A, const bf16_t* __restrict__ W,
                                                         const TR* __restrict__ R, TC* __restrict__ C, int M, int N,
-                                                        int K, int tiles_n, int group, int splits) {
+                                                        int K, int tiles_n, int group, int splits,
+                                                        typename Operand<TE>::Scales sc) {
   using namespace tile;
+  using Op = Operand<TE>;
+  constexpr bool I8 = Op::kInt8;
+  const int KT = I8 ? (K + BK - 1) / BK : K / 64;  // W tiles along K
   using G = Geo<QM, QN, NS>;
   constexpr int BM = G::BM, BN = G::BN, STAGE = G::STAGE, A_LOADS = G::A_LOADS, B_LOADS = G::B_LOADS, LOADS = G::LOADS;
   constexpr int MF = G::MF, RD = G::RD;
@@ -210,13 +259,14 @@ __global__ __launch_bounds__(256) void gemm_tile_kernel(const bf16_t* __restrict
 #pragma unroll
   for (int i = 0; i < B_LOADS; ++i) {  // tiled W: rows of 64-row block row/64, k-tile added per stage
     const int row = (wave * B_LOADS + i) * RPL + lrow;
-    boff[i] = ((uint32_t)(row >> 6) * (K / 64) * kWTileElts + (row & 63) * 64 + (lpos ^ ((row >> 1) & 7)) * 8) * 2;
+    boff[i] = ((uint32_t)(row >> 6) * KT * kWTileElts + (row & 63) * 64 + (lpos ^ ((row >> 1) & 7)) * 8) * 2;
   }
   static_assert(BK == kWTile, "one W tile per stage");
   const __amdgpu_buffer_rsrc_t rA = buffer_rsrc(A + (long)m0 * K, (uint32_t)min(M - m0, BM) * K * 2);
+  const int w_blocks = I8 ? min(BN, N - n0) / 64 : BN / 64;  // reads past them give zero
   const __amdgpu_buffer_rsrc_t rW =
-      buffer_rsrc(W + (long)(n0 >> 6) * (K / 64) * kWTileElts, (uint32_t)(BN / 64) * (K / 64) * kWTileElts * 2);
-  const int T_all = K / BK;
+      buffer_rsrc(W + (long)(n0 >> 6) * KT * kWTileElts, (uint32_t)w_blocks * KT * kWTileElts * 2);
+  const int T_all = KT;
   const int st0 = ks * T_all / splits, T = (ks + 1) * T_all / splits - st0;  // this workgroup's stages
   // DMA instruction l (0..LOADS-1) of stage s into slot dslot (= s % NS);
   // the stage's step rides in the scalar offset
@@ -232,32 +282,32 @@ __global__ __launch_bounds__(256) void gemm_tile_kernel(const bf16_t* __restrict
   // 32x32x16 operands: lane (h, r) holds row r of a 32-row block, k 8h..8h+7
   // of a 16-k slice; fragments double-buffered by slice parity
   const int h = lane >> 5, r32 = lane & 31;
-  bf16x8_t fa[2][QM], fb[2][QN];
+  using Frag = typename Op::Frag;
+  Frag fa[2][QM], fb[2][QN];
   // fragment r (0..QM+QN-1) of slice sl, in first-use order: a0 b0 .. b(QN-1) a1 .. a(QM-1)
   auto read_frag = [&](int slot, int sl, int r) __attribute__((always_inline)) {
     const bf16_t* a = smem + slot * STAGE;
     if (r == 0)
-      fa[sl & 1][0] = __builtin_bit_cast(bf16x8_t, *(const uint4*)(a + swz(wm * 32 * QM + r32, 2 * sl + h)));
+      fa[sl & 1][0] = __builtin_bit_cast(Frag, *(const uint4*)(a + swz(wm * 32 * QM + r32, 2 * sl + h)));
     else if (r <= QN)
       fb[sl & 1][r - 1] = __builtin_bit_cast(
-          bf16x8_t, *(const uint4*)(a + G::A_ELTS + swz(wn * 32 * QN + (r - 1) * 32 + r32, 2 * sl + h)));
+          Frag, *(const uint4*)(a + G::A_ELTS + swz(wn * 32 * QN + (r - 1) * 32 + r32, 2 * sl + h)));
     else
       fa[sl & 1][r - QN] =
-          __builtin_bit_cast(bf16x8_t, *(const uint4*)(a + swz(wm * 32 * QM + (r - QN) * 32 + r32, 2 * sl + h)));
+          __builtin_bit_cast(Frag, *(const uint4*)(a + swz(wm * 32 * QM + (r - QN) * 32 + r32, 2 * sl + h)));
   };
-  f32x16_t acc[QM][QN];
+  typename Op::Acc16 acc[QM][QN];
 #pragma unroll
   for (int i = 0; i < QM; ++i)
 #pragma unroll
     for (int j = 0; j < QN; ++j)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
   // an (empty) AGPR operand makes the compiler select the AGPR form of the
   // MFMAs, which keeps the accumulators in place in the AGPR file
   asm volatile("" ::"a"(0.f));
   auto mfma = [&](int sl, int q) __attribute__((always_inline)) {
-    acc[q / QN][q % QN] =
-        __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[sl & 1][q / QN], fb[sl & 1][q % QN], acc[q / QN][q % QN], 0, 0, 0);
+    acc[q / QN][q % QN] = Op::mfma32(fa[sl & 1][q / QN], fb[sl & 1][q % QN], acc[q / QN][q % QN]);
   };
 
   // stage st, in LDS slot st % NS. `slotc`: that slot as an integral constant
@@ -379,22 +429,46 @@ __global__ __launch_bounds__(256) void gemm_tile_kernel(const bf16_t* __restrict
 #pragma unroll
       for (int pass = 0; pass < NPASS; ++pass) {
         const int row = rbase + i * 32 + pass * RPP + lane / LPR, oc = (lane % LPR) * V;
-        const long idx = (long)min(row, M - 1) * ldc + ccol + oc;  // rows past M: a valid row, result unused
+        long idx = (long)min(row, M - 1) * ldc + ccol + oc;  // rows past M: a valid row, result unused
+        if constexpr (I8) idx = (long)min(row, M - 1) * ldc + min(ccol + oc, ldc - V);  // and columns past N
 #pragma unroll
         for (int q = 0; q < RCH; ++q) rr[i & 1][pass][q] = *(const RRaw*)(R + idx + q * 4);
       }
     }
   };
+  // int8: this lane's column scales (its columns are the same in every pass)
+  // and, a block ahead like the residual, its rows' scales
+  float swv[I8 ? (EPI == 2 ? 2 : 1) : 1][I8 ? V : 1], sav[2][I8 ? NPASS : 1];
+  auto load_sa = [&](int i) __attribute__((always_inline)) {
+    if constexpr (I8) {
+#pragma unroll
+      for (int pass = 0; pass < NPASS; ++pass) sav[i & 1][pass] = sc.row[min(rbase + i * 32 + pass * RPP + lane / LPR, M - 1)];
+    }
+  };
+  if constexpr (I8) {
+    const int oc = (lane % LPR) * V;
+    const int col = EPI == 2 ? cbase + oc / 32 * 64 + oc % 32 : cbase + oc;
+#pragma unroll
+    for (int e = 0; e < V; e += 4) {
+      const float4 w4 = *(const float4*)(sc.col + min(col, N - V) + e);
+      swv[0][e] = w4.x, swv[0][e + 1] = w4.y, swv[0][e + 2] = w4.z, swv[0][e + 3] = w4.w;
+      if constexpr (EPI == 2) {
+        const float4 u4 = *(const float4*)(sc.col + min(col + 32, N - V) + e);
+        swv[1][e] = u4.x, swv[1][e + 1] = u4.y, swv[1][e + 2] = u4.z, swv[1][e + 3] = u4.w;
+      }
+    }
+  }
   load_r(0);
+  load_sa(0);
   lds_barrier_pinned();  // every wave is done reading operand slots
   float* stg = (float*)smem + wave * (32 * ROWF);
 #pragma unroll
   for (int i = 0; i < QM; ++i) {
-    if (i + 1 < QM) load_r(i + 1);
+    if (i + 1 < QM) load_r(i + 1), load_sa(i + 1);
 #pragma unroll
     for (int j = 0; j < QN; ++j)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) stg[(8 * (r >> 2) + 4 * h + (r & 3)) * ROWF + j * 32 + r32] = acc[i][j][r];
+      for (int r = 0; r < 16; ++r) stg[(8 * (r >> 2) + 4 * h + (r & 3)) * ROWF + j * 32 + r32] = (float)acc[i][j][r];
     // LDS accesses of one wave complete in order: the reads below see the writes
 #pragma unroll
     for (int pass = 0; pass < NPASS; ++pass) {
@@ -406,7 +480,12 @@ __global__ __launch_bounds__(256) void gemm_tile_kernel(const bf16_t* __restrict
         const float* g = stg + lr * ROWF + p * 64 + c;
 #pragma unroll
         for (int e = 0; e < V; e += 4) {
-          const float4 gv = *(const float4*)(g + e), uv = *(const float4*)(g + 32 + e);
+          float4 gv = *(const float4*)(g + e), uv = *(const float4*)(g + 32 + e);
+          if constexpr (I8) {
+            const float f = sav[i & 1][pass];
+            gv.x *= f * swv[0][e], gv.y *= f * swv[0][e + 1], gv.z *= f * swv[0][e + 2], gv.w *= f * swv[0][e + 3];
+            uv.x *= f * swv[1][e], uv.y *= f * swv[1][e + 1], uv.z *= f * swv[1][e + 2], uv.w *= f * swv[1][e + 3];
+          }
           v[e] = silu_fast(gv.x) * uv.x;
           v[e + 1] = silu_fast(gv.y) * uv.y;
           v[e + 2] = silu_fast(gv.z) * uv.z;
@@ -420,6 +499,10 @@ __global__ __launch_bounds__(256) void gemm_tile_kernel(const bf16_t* __restrict
           v[e + 1] = a4.y;
           v[e + 2] = a4.z;
           v[e + 3] = a4.w;
+        }
+        if constexpr (I8) {
+#pragma unroll
+          for (int e = 0; e < V; ++e) v[e] *= sav[i & 1][pass] * swv[0][e];
         }
       }
       if constexpr (EPI == 1) {
@@ -445,7 +528,7 @@ __global__ __launch_bounds__(256) void gemm_tile_kernel(const bf16_t* __restrict
           v[3] += bf_hi(rr[i & 1][pass][0].y);
         }
       }
-      if (row >= M) continue;
+      if (row >= M || (I8 && ccol + oc >= ldc)) continue;
       const long idx = (long)row * ldc + ccol + oc;
       if constexpr (std::is_same<TC, bf16_t>::value) {
         typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -464,15 +547,59 @@ template <int QM, int QN, int NS, bool NT, int EPI, typename TR, typename TC>
 int launch_tile_g(int M, int N, int cols, int K, const void* A, const void* W, const void* R, void* C, hipStream_t st,
                   int splits, int group) {
   using G = tile::Geo<QM, QN, NS>;
-  static const hipError_t attr = hipFuncSetAttribute((const void*)gemm_tile_kernel<QM, QN, NS, NT, EPI, TR, TC>,
+  static const hipError_t attr = hipFuncSetAttribute((const void*)gemm_tile_kernel<bf16_t, QM, QN, NS, NT, EPI, TR, TC>,
                                                      hipFuncAttributeMaxDynamicSharedMemorySize, (int)G::LDS_BYTES);
   if (attr != hipSuccess) return -1;
   const int tiles_m = (M + G::BM - 1) / G::BM, tiles_n = cols / G::BN;
-  hipLaunchKernelGGL((gemm_tile_kernel<QM, QN, NS, NT, EPI, TR, TC>), dim3(tiles_m * tiles_n * splits), dim3(tile::NT),
+  hipLaunchKernelGGL((gemm_tile_kernel<bf16_t, QM, QN, NS, NT, EPI, TR, TC>), dim3(tiles_m * tiles_n * splits), dim3(tile::NT),
                      G::LDS_BYTES, st, (const bf16_t*)A, (const bf16_t*)W, (const TR*)R, (TC*)C, M, N, K, tiles_n,
-                     group, splits);
+                     group, splits, NoScales{});
   return 0;
 }
+
+// The int8 form; N may end inside the last tile.
+template <int QM, int QN, int NS, bool NT, int EPI, typename TR, typename TC>
+int launch_tile_i8(int M, int N, int cols, int K, const void* A, const float* sa, const void* W, const float* sw,
+                   const void* R, void* C, hipStream_t st, int group) {
+  using G = tile::Geo<QM, QN, NS>;
+  static const hipError_t attr = hipFuncSetAttribute((const void*)gemm_tile_kernel<int8_t, QM, QN, NS, NT, EPI, TR, TC>,
+                                                     hipFuncAttributeMaxDynamicSharedMemorySize, (int)G::LDS_BYTES);
+  if (attr != hipSuccess) return -1;
+  const int tiles_m = (M + G::BM - 1) / G::BM, tiles_n = (cols + G::BN - 1) / G::BN;
+  hipLaunchKernelGGL((gemm_tile_kernel<int8_t, QM, QN, NS, NT, EPI, TR, TC>), dim3(tiles_m * tiles_n), dim3(tile::NT),
+                     G::LDS_BYTES, st, (const bf16_t*)A, (const bf16_t*)W, (const TR*)R, (TC*)C, M, N, K, tiles_n, group, 1,
+                     I8Scales{sa, sw});
+  return 0;
+}
+
+// The tile kernel's shapes. `start` and `stage` are microseconds of one
+// workgroup alone on its compute unit: prologue + epilogue, and one 64-k
+// stage. Least-squares fits over the 8B and 70B layers' GEMMs at 80 to 4096
+// rows and 1 to 4 K splits, weights cold in every cache (rms error 7-16%; the
+// shape and splits chosen are within 1% of the best measured on average, 14%
+// at worst). Per output element a larger tile is cheaper (256x256: 1.26 us per
+// stage for four 128x128 tiles' work at 0.47 each) but fills fewer compute units.
+struct TileCfg {
+  int qm, qn;  // 64 qm x 64 qn outputs per workgroup
+  float start, stage;
+};
+constexpr TileCfg kTileCfgs[] = {
+    {4, 4, 13.7f, 1.260f}, {3, 4, 10.7f, 1.127f}, {2, 4, 10.3f, 0.735f}, {4, 2, 10.6f, 0.715f},
+    {3, 2, 7.6f, 0.571f},  {2, 2, 7.4f, 0.466f},  {2, 1, 6.0f, 0.326f},  {1, 1, 4.0f, 0.250f},
+};
+constexpr int kTileCfgCount = sizeof(kTileCfgs) / sizeof(kTileCfgs[0]);
+
+// One tile row: weight loads with the non-temporal hint (see the kernel).
+// Two rows of 192x256 or 256x256 tiles gain too (us, N 57344, K 8192: 300
+// rows 358 -> 348, 512 rows 418 -> 401; N 28672, K 4096 at 389 102 -> 99).
+// Otherwise workgroups that share weights drift apart where the last tile row
+// is short, and the hint costs up to 20% (N 4096, K 14336 at 300 rows: 70, with
+// it 88), and from four rows on it gives nothing or loses 1 to 7%.
+inline bool tile_nt(int M, const TileCfg& t) { return M <= 64 * t.qm * (t.qm >= 3 && t.qn == 4 ? 2 : 1); }
+
+// See their definitions in k_gemm.hip.
+int tile_columns(int M, int N, int K, bool swiglu, const TilePlan& whole, TilePlan* first, TilePlan* rest);
+int tile_group(int M, int N, int qm);
 
 // Every instance the launcher reaches, X(QM, QN, NS, NT, EPI, TR, TC), by the
 // source file that compiles it. NS: ring slots that fit 160 KiB of LDS.
@@ -500,5 +627,31 @@ int launch_tile_g(int M, int N, int cols, int K, const void* A, const void* W, c
 #define PS_TILE_INSTANTIATE(QM, QN, NS, NT, EPI, TR, TC)                                                        \
   template int launch_tile_g<QM, QN, NS, NT, EPI, TR, TC>(int, int, int, int, const void*, const void*,         \
                                                           const void*, void*, hipStream_t, int, int);
+
+// int8: the same shapes, and every combination of types in all of them where a
+// layer's products have it.
+#define PS_I8_INSTANCES_NT(X, QM, QN, NS, NT)                                                                \
+  X(QM, QN, NS, NT, 0, float, bf16_t) X(QM, QN, NS, NT, 0, float, float) X(QM, QN, NS, NT, 1, bf16_t, float) \
+  X(QM, QN, NS, NT, 1, float, bf16_t) X(QM, QN, NS, NT, 1, bf16_t, bf16_t)
+#define PS_I8_INSTANCES_ALL(X, QM, QN, NS) \
+  PS_I8_INSTANCES_NT(X, QM, QN, NS, false) PS_I8_INSTANCES_NT(X, QM, QN, NS, true)
+#define PS_I8_INSTANCES_256(X)                                                      \
+  PS_I8_INSTANCES_ALL(X, 4, 4, 2) PS_TILE_INSTANCES_SWIGLU(X, 4, 4, 2)             \
+  X(4, 4, 2, false, 1, float, float) X(4, 4, 2, false, 2, float, float)
+#define PS_I8_INSTANCES_WIDE(X)                                                    \
+  PS_I8_INSTANCES_ALL(X, 3, 4, 2) PS_TILE_INSTANCES_SWIGLU(X, 3, 4, 2)             \
+  PS_I8_INSTANCES_ALL(X, 2, 4, 3) PS_TILE_INSTANCES_SWIGLU(X, 2, 4, 3)
+#define PS_I8_INSTANCES_TALL(X)                                                    \
+  PS_I8_INSTANCES_ALL(X, 4, 2, 3) PS_TILE_INSTANCES_SWIGLU(X, 4, 2, 3)             \
+  PS_I8_INSTANCES_ALL(X, 3, 2, 3) PS_TILE_INSTANCES_SWIGLU(X, 3, 2, 3)
+#define PS_I8_INSTANCES_SMALL(X)                                                   \
+  PS_I8_INSTANCES_ALL(X, 2, 2, 4) PS_TILE_INSTANCES_SWIGLU(X, 2, 2, 4)             \
+  PS_I8_INSTANCES_ALL(X, 2, 1, 6) PS_I8_INSTANCES_NT(X, 1, 1, 5, false)
+#define PS_I8_INSTANCES(X) \
+  PS_I8_INSTANCES_256(X) PS_I8_INSTANCES_WIDE(X) PS_I8_INSTANCES_TALL(X) PS_I8_INSTANCES_SMALL(X)
+#define PS_I8_INSTANTIATE(QM, QN, NS, NT, EPI, TR, TC)                                                          \
+  template int launch_tile_i8<QM, QN, NS, NT, EPI, TR, TC>(int, int, int, int, const void*, const float*,       \
+                                                           const void*, const float*, const void*, void*,      \
+                                                           hipStream_t, int);
 
 }  // namespace ps

@@ -7,7 +7,7 @@
 //
 //  * gemm_tile_kernel (gemm_tile.h): M > 64, 256x256 down to 64x64 workgroup
 //    tiles chosen by gemm_tile_plan.
-//  * gemm_skinny_kernel: decode-sized M (<= 64). Streams W once from HBM
+//  * gemm_skinny_kernel (gemm_skinny.h): decode-sized M (<= 64). Streams W once from HBM
 //    with 16-byte loads, one 16-column MFMA block per wave, activations
 //    staged in LDS and shared by the workgroup's four waves; K may be split
 //    across workgroups, fp32 partials then reduced in split order by
@@ -16,184 +16,12 @@
 //
 // Epilogues: store, residual add (C = R + A W^T) and SwiGLU (W rows
 // interleaved gate/up in blocks of 32; C[:, j] = silu(gate_j) * up_j).
+#include "gemm_skinny.h"
 #include "gemm_tile.h"
 
 #include <mutex>
 
 namespace ps {
-
-// ==================================================================== skinny
-// Decode-sized M (<= 64): the weight stream is the whole cost (AI = M
-// FLOP/byte). A workgroup owns 64 WN weight rows (output columns, WN 1, 2 or 4) and a K
-// range; its four waves own 16 WN rows each. Stages of 64 k hold the
-// activation tile [16 MB rows][64] and the weight tile [64 WN rows][64];
-// both are filled by global->LDS DMA into an NS-deep ring, so the bytes in
-// flight cost no registers, and one barrier per stage recycles the slot.
-// LDS rows are 128 B with 16-byte chunks XOR-swizzled by row % 8 (the DMA
-// lane order is chosen so the fill lands swizzled). Per 32-wide k step a
-// wave does MB x WN v_mfma_f32_16x16x32_bf16 with A = activations, B = W.
-// With one K split the epilogue is applied from registers; otherwise fp32
-// partials go to the workspace and gemm_reduce_kernel sums them in split
-// order.
-namespace skinny {
-constexpr int NT = 256;
-constexpr int KS = 64;    // k per stage
-constexpr int MAXM = 64;
-template <int WN>
-constexpr int ring() { return WN == 4 ? 3 : 4; }  // stages; three of the widest are as many bytes in flight as six of 128 rows
-template <int MB, int WN>
-constexpr size_t lds_bytes() { return (size_t)ring<WN>() * (16 * MB + 64 * WN) * KS * 2; }
-}  // namespace skinny
-
-template <int MB, int WN, int EPI, typename TR, typename TC, bool DIRECT>
-__global__ __launch_bounds__(256) void gemm_skinny_kernel(const bf16_t* __restrict__ A, const bf16_t* __restrict__ W,
-                                                          float* __restrict__ part, const TR* __restrict__ R,
-                                                          TC* __restrict__ C, int M, int N, int K, int S) {
-  using namespace skinny;
-  static_assert(!(DIRECT && EPI == 2) || WN >= 2, "in-kernel SwiGLU pairs gate and up blocks per wave");
-  constexpr int NS = ring<WN>();
-  static_assert(KS == kWTile, "one W tile per stage");
-  constexpr int AROWS = 16 * MB, WROWS = 64 * WN;
-  constexpr int STAGE = (AROWS + WROWS) * KS;  // bf16 elements
-  constexpr int TA = AROWS / 8;                // A DMA instructions per stage (8 rows each), round-robin
-  constexpr int WI = WROWS / 8 / 4;            // W DMA instructions per wave per stage
-  extern __shared__ __attribute__((aligned(16))) bf16_t smem[];
-  const int n0 = blockIdx.x * WROWS;
-  const int split = blockIdx.y;
-  // split `split` of S takes 64-k stages [split TT / S, (split + 1) TT / S): near-equal ranges for any S
-  const int TT = K / KS;
-  const int st0 = split * TT / S;
-  const int T = (split + 1) * TT / S - st0;
-  const int kb = st0 * KS;
-  const int kps = T * KS;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
-  const int g = lane >> 4, c = lane & 15;
-  // DMA lane mapping: an instruction fills 8 rows; lane l lands in row l/8 at
-  // chunk l%8, which holds global chunk (l%8) ^ (row%8)
-  const int drow = lane >> 3, dch = (lane & 7) ^ (lane >> 3);
-  const int n_ai = (TA - wave + 3) / 4;  // this wave's A instructions (0..2)
-  // DMA sources: buffer resources at the split's first activation column and
-  // at the workgroup's first W tile of the split, 32-bit lane byte offsets
-  const __amdgpu_buffer_rsrc_t rA = buffer_rsrc(A + kb, (uint32_t)((long)(M - 1) * K + kps) * 2);
-  const __amdgpu_buffer_rsrc_t rW = buffer_rsrc(W + ((long)(n0 >> 6) * (K / 64) + kb / 64) * kWTileElts,
-                                                (uint32_t)((WN - 1) * (K / 64) + kps / 64) * kWTileElts * 2);
-  uint32_t aoff[2], woff[WI];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int row = (wave + 4 * i) * 8 + drow;
-    aoff[i] = ((uint32_t)min(row, M - 1) * K + dch * 8) * 2;
-  }
-  // tiled W: the stage's 64 k of each 64-row block is one contiguous tile
-#pragma unroll
-  for (int i = 0; i < WI; ++i) {
-    const int r = (wave * WI + i) * 8 + drow;  // row within the workgroup's WN blocks
-    woff[i] = ((uint32_t)(r >> 6) * (K / 64) * kWTileElts + (r & 63) * 64 + dch * 8) * 2;
-  }
-  auto dma = [&](int t, int slot) {
-    bf16_t* st = smem + slot * STAGE;
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      if (i < n_ai) load_lds16_buf(rA, aoff[i] + t * KS * 2, st + (wave + 4 * i) * 8 * KS);
-#pragma unroll
-    for (int i = 0; i < WI; ++i) load_lds16_buf_nt(rW, woff[i] + t * kWTileElts * 2, st + AROWS * KS + (wave * WI + i) * 8 * KS);
-  };
-  // this wave's own fills older than the most recent stage have landed
-  auto wait_prev_stage = [&]() {
-    if (n_ai == 2) wait_vmcnt_lgkm0<(NS - 2) * (WI + 2)>();
-    else if (n_ai == 1) wait_vmcnt_lgkm0<(NS - 2) * (WI + 1)>();
-    else wait_vmcnt_lgkm0<(NS - 2) * WI>();
-  };
-  auto swz = [](int row, int ch) { return row * KS + ((ch ^ (row & 7)) << 3); };
-  // weight rows of n-block nb for this wave; for SwiGLU with WN 2 block 0 is a
-  // gate block and block 1 the matching up block of the 32-row interleave, with
-  // WN 4 a wave's blocks 0, 1 are gate and 2, 3 up as they lie
-  auto wrow = [&](int nb) {
-    if constexpr (EPI == 2 && WN == 2) {
-      const int q = wave >> 1, h = wave & 1;
-      return 64 * q + 32 * nb + 16 * h + c;
-    } else {
-      return wave * 16 * WN + nb * 16 + c;
-    }
-  };
-  f32x4_t acc[WN][MB];
-#pragma unroll
-  for (int nb = 0; nb < WN; ++nb)
-#pragma unroll
-    for (int i = 0; i < MB; ++i) acc[nb][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  auto compute = [&](int slot) {
-    const bf16_t* st = smem + slot * STAGE;
-    const bf16_t* wt = st + AROWS * KS;
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      bf16x8_t wf[WN];
-#pragma unroll
-      for (int nb = 0; nb < WN; ++nb) wf[nb] = __builtin_bit_cast(bf16x8_t, *(const uint4*)(wt + swz(wrow(nb), 4 * j + g)));
-#pragma unroll
-      for (int i = 0; i < MB; ++i) {
-        const bf16x8_t af = __builtin_bit_cast(bf16x8_t, *(const uint4*)(st + swz(16 * i + c, 4 * j + g)));
-#pragma unroll
-        for (int nb = 0; nb < WN; ++nb)
-          acc[nb][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(af, wf[nb], acc[nb][i], 0, 0, 0);
-      }
-    }
-  };
-#pragma unroll
-  for (int d = 0; d < NS - 1; ++d)
-    if (d < T) dma(d, d);
-  int slot = 0, fill = NS - 1, t = 0;
-  // steady state: every stage refills the slot freed by the previous one
-  for (; t + NS - 1 < T; ++t) {
-    wait_prev_stage();
-    lds_barrier();
-    dma(t + NS - 1, fill);
-    compute(slot);
-    if (++slot == NS) slot = 0;
-    if (++fill == NS) fill = 0;
-  }
-  for (; t < T; ++t) {  // drain
-    wait_vmcnt_lgkm0<0>();
-    lds_barrier();
-    compute(slot);
-    if (++slot == NS) slot = 0;
-  }
-  // acc[nb][i][r] = C[16i + 4g + r][n0 + wrow(nb)]
-  if constexpr (DIRECT) {
-#pragma unroll
-    for (int i = 0; i < MB; ++i)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int row = 16 * i + 4 * g + r;
-        if (row >= M) continue;
-        if constexpr (EPI == 2) {
-#pragma unroll
-          for (int nb = 0; nb < WN / 2; ++nb) {
-            const int col = n0 / 2 + (WN == 4 ? 32 * wave + 16 * nb : 16 * wave) + c;
-            st_elt<TC>(C, (long)row * (N / 2) + col, silu_fast(acc[nb][i][r]) * acc[nb + WN / 2][i][r]);
-          }
-        } else {
-#pragma unroll
-          for (int nb = 0; nb < WN; ++nb) {
-            const long idx = (long)row * N + n0 + wrow(nb);
-            float v = acc[nb][i][r];
-            if constexpr (EPI == 1) v += ld_elt<TR>(R, idx);
-            st_elt<TC>(C, idx, v);
-          }
-        }
-      }
-  } else {
-    float* pp = part + (long)split * M * N;
-#pragma unroll
-    for (int nb = 0; nb < WN; ++nb)
-#pragma unroll
-      for (int i = 0; i < MB; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int row = 16 * i + 4 * g + r;
-          if (row < M) pp[(long)row * N + n0 + wrow(nb)] = acc[nb][i][r];
-        }
-  }
-}
 
 // Sum split partials in split order, then apply the epilogue.
 template <int EPI, typename TR, typename TC>
@@ -432,23 +260,6 @@ int compute_units() {
   return n;
 }
 
-// The tile kernel's shapes. `start` and `stage` are microseconds of one
-// workgroup alone on its compute unit: prologue + epilogue, and one 64-k
-// stage. Least-squares fits over the 8B and 70B layers' GEMMs at 80 to 4096
-// rows and 1 to 4 K splits, weights cold in every cache (rms error 7-16%; the
-// shape and splits chosen are within 1% of the best measured on average, 14%
-// at worst). Per output element a larger tile is cheaper (256x256: 1.26 us per
-// stage for four 128x128 tiles' work at 0.47 each) but fills fewer compute units.
-struct TileCfg {
-  int qm, qn;  // 64 qm x 64 qn outputs per workgroup
-  float start, stage;
-};
-constexpr TileCfg kTileCfgs[] = {
-    {4, 4, 13.7f, 1.260f}, {3, 4, 10.7f, 1.127f}, {2, 4, 10.3f, 0.735f}, {4, 2, 10.6f, 0.715f},
-    {3, 2, 7.6f, 0.571f},  {2, 2, 7.4f, 0.466f},  {2, 1, 6.0f, 0.326f},  {1, 1, 4.0f, 0.250f},
-};
-constexpr int kTileCfgCount = sizeof(kTileCfgs) / sizeof(kTileCfgs[0]);
-
 // Cost in microseconds of a tile-kernel launch: rounds of workgroups over the
 // compute units (one resident per unit), the weight stream (5 TB/s) that the
 // rounds cannot beat and only partly hide, and the split partials (fp32,
@@ -504,7 +315,7 @@ TilePlan gemm_tile_plan(int M, int N, int K, int max_splits, bool swiglu, double
 // 702; N 10240, K 8192 at 2048 296 -> 268; N 6144, K 4096 at 3500 144 -> 139.
 // Where it promised 4 to 5% it gave 1 or 2, once -2. Beside another stream's
 // attention it loses (mixed step of 4 x 512 + 32 rows 1074 -> 1081).
-static int tile_columns(int M, int N, int K, bool swiglu, const TilePlan& whole, TilePlan* first, TilePlan* rest) {
+int tile_columns(int M, int N, int K, bool swiglu, const TilePlan& whole, TilePlan* first, TilePlan* rest) {
   const long cu = compute_units();
   auto wgs = [&](const TileCfg& t, int n) { return (long)((M + 64 * t.qm - 1) / (64 * t.qm)) * (n / (64 * t.qn)); };
   if (whole.s != 1 || wgs(kTileCfgs[whole.cfg], N) <= cu) return 0;
@@ -548,7 +359,7 @@ size_t TilePartials::bytes(int max_rows) const {
 // of equal size of at most ~1280 rows, so that the workgroups sharing a
 // weight column run together and no short group trails; more rows: 8 tile
 // rows of 256 on wide outputs (more W reuse per XCD), 4 on narrow ones.
-static int tile_group(int M, int N, int qm) {
+int tile_group(int M, int N, int qm) {
   const int tiles_m = (M + 64 * qm - 1) / (64 * qm);
   if (M <= 2304) {
     const int groups = (tiles_m * 64 * qm + 1279) / 1280;
@@ -574,14 +385,7 @@ template <int EPI, typename TR, typename TC>
 static int launch_tile_cols(int M, int N, int cols, int K, TilePlan pl, const void* A, const void* W, const void* R,
                             void* C, hipStream_t st) {
   const int group = tile_group(M, cols, kTileCfgs[pl.cfg].qm);
-  // One tile row: weight loads with the non-temporal hint (see the kernel).
-  // Two rows of 192x256 or 256x256 tiles gain too (us, N 57344, K 8192: 300
-  // rows 358 -> 348, 512 rows 418 -> 401; N 28672, K 4096 at 389 102 -> 99).
-  // Otherwise workgroups that share weights drift apart where the last tile row
-  // is short, and the hint costs up to 20% (N 4096, K 14336 at 300 rows: 70, with
-  // it 88), and from four rows on it gives nothing or loses 1 to 7%.
-  const TileCfg& tc = kTileCfgs[pl.cfg];
-  const bool nt = M <= 64 * tc.qm * (tc.qm >= 3 && tc.qn == 4 ? 2 : 1);
+  const bool nt = tile_nt(M, kTileCfgs[pl.cfg]);
 #define PS_TILE_GO(QM, QN, NS, NT) launch_tile_g<QM, QN, NS, NT, EPI, TR, TC>(M, N, cols, K, A, W, R, C, st, pl.s, group)
 #define PS_TILE_GO_NT(QM, QN, NS) (nt ? PS_TILE_GO(QM, QN, NS, true) : PS_TILE_GO(QM, QN, NS, false))
   if constexpr (kTileAllShapes<EPI, TR, TC>) {
@@ -724,10 +528,10 @@ static int launch_skinny_k(int M, int N, int K, int S, const void* A, const void
                            void* C, hipStream_t st) {
   constexpr size_t lds = skinny::lds_bytes<MB, WN>();
   static const hipError_t attr = hipFuncSetAttribute(
-      (const void*)gemm_skinny_kernel<MB, WN, EPI, TR, TC, DIRECT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+      (const void*)gemm_skinny_kernel<bf16_t, MB, WN, EPI, TR, TC, DIRECT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (attr != hipSuccess) return -1;
-  hipLaunchKernelGGL((gemm_skinny_kernel<MB, WN, EPI, TR, TC, DIRECT>), dim3(N / (64 * WN), S), dim3(skinny::NT), lds,
-                     st, (const bf16_t*)A, (const bf16_t*)W, part, (const TR*)R, (TC*)C, M, N, K, S);
+  hipLaunchKernelGGL((gemm_skinny_kernel<bf16_t, MB, WN, EPI, TR, TC, DIRECT>), dim3(N / (64 * WN), S), dim3(skinny::NT), lds,
+                     st, (const bf16_t*)A, (const bf16_t*)W, part, (const TR*)R, (TC*)C, M, N, K, S, NoScales{});
   return 0;
 }
 

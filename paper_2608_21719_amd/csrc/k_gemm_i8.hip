@@ -1,0 +1,199 @@
+// int8 GEMM: C[m, n] = epilogue(s_m w_n sum_k A[m, k] W[n, k]), int8 operands, int32
+// sums, a scale for each row of A (token) and each row of W (output channel). The
+// sums are exact (K < 2^17), so a result does not depend on tile shapes or splits.
+//
+// The kernels are the bf16 GEMMs' with int8 operands (Operand<int8_t>): W lies in
+// 64 x 128 tiles of the same 8 KiB, an MFMA takes the same 16 bytes per lane for
+// twice the k. So a launch costs what a bf16 launch of half the K costs, and the
+// plans (tile shape, weight blocks, K splits) are taken for that.
+#include "gemm_skinny.h"
+
+namespace ps {
+
+#define PS_I8_EXTERN(QM, QN, NS, NT, EPI, TR, TC)                                                                 \
+  extern template int launch_tile_i8<QM, QN, NS, NT, EPI, TR, TC>(int, int, int, int, const void*, const float*,  \
+                                                                  const void*, const float*, const void*, void*, \
+                                                                  hipStream_t, int);
+PS_I8_INSTANCES(PS_I8_EXTERN)
+#undef PS_I8_EXTERN
+
+namespace {
+
+struct Args {
+  int M, N, K;  // K in pairs
+  const void* a;
+  const float* sa;
+  const void* w;
+  const float* sw;
+  const void* r;
+  void* c;
+  hipStream_t st;
+};
+
+int pad(int x, int to) { return (x + to - 1) / to * to; }
+
+// ---------------------------------------------------------------- tiles, M > 64
+template <int EPI, typename TR, typename TC>
+constexpr bool kAllShapes = !(EPI != 0 && std::is_same<TR, float>::value && std::is_same<TC, float>::value);
+
+template <int EPI, typename TR, typename TC>
+int tile_cols(const Args& x, int cols, TilePlan pl) {
+  const int group = tile_group(x.M, cols, kTileCfgs[pl.cfg].qm);
+  const bool nt = tile_nt(x.M, kTileCfgs[pl.cfg]);
+#define PS_I8_GO(QM, QN, NS, NT) \
+  launch_tile_i8<QM, QN, NS, NT, EPI, TR, TC>(x.M, x.N, cols, x.K, x.a, x.sa, x.w, x.sw, x.r, x.c, x.st, group)
+#define PS_I8_GO_NT(QM, QN, NS) (nt ? PS_I8_GO(QM, QN, NS, true) : PS_I8_GO(QM, QN, NS, false))
+  if constexpr (kAllShapes<EPI, TR, TC>) {
+    switch (pl.cfg) {
+      case 0: return PS_I8_GO_NT(4, 4, 2);
+      case 1: return PS_I8_GO_NT(3, 4, 2);
+      case 2: return PS_I8_GO_NT(2, 4, 3);
+      case 3: return PS_I8_GO_NT(4, 2, 3);
+      case 4: return PS_I8_GO_NT(3, 2, 3);
+      case 5: return PS_I8_GO_NT(2, 2, 4);
+      default: break;
+    }
+    if constexpr (EPI != 2) {
+      if (pl.cfg == 6) return PS_I8_GO_NT(2, 1, 6);
+      if (pl.cfg == 7) return PS_I8_GO(1, 1, 5, false);  // M > 64: two tile rows at least
+    }
+    return -1;
+  } else {
+    return PS_I8_GO(4, 4, 2, false);
+  }
+#undef PS_I8_GO_NT
+#undef PS_I8_GO
+}
+
+template <int EPI, typename TR, typename TC>
+int launch_tiles(const Args& x) {
+  const int kp = pad(x.K, tile::BK);
+  const TilePlan pl = gemm_tile_plan(x.M, pad(x.N, 256), kp, 1, EPI == 2);
+  TilePlan first, rest;
+  const int n = kAllShapes<EPI, TR, TC> && x.N % 256 == 0 ? tile_columns(x.M, x.N, kp, EPI == 2, pl, &first, &rest) : 0;
+  if (n == 0) return tile_cols<EPI, TR, TC>(x, x.N, pl);
+  if (tile_cols<EPI, TR, TC>(x, n, first)) return -1;
+  Args y = x;
+  y.w = (const bf16_t*)x.w + (long)(n / 64) * (kp / 64) * kWTileElts;
+  y.sw = x.sw + n;
+  y.r = x.r ? (const TR*)x.r + n : nullptr;
+  y.c = (TC*)x.c + (EPI == 2 ? n / 2 : n);
+  return tile_cols<EPI, TR, TC>(y, x.N - n, rest);
+}
+
+// --------------------------------------------------------------- skinny, M <= 64
+// Sums the splits' int32 partials and applies scales and epilogue, four columns
+// per thread.
+template <int EPI, typename TR, typename TC>
+__global__ __launch_bounds__(256) void gemm_i8_reduce_kernel(const int* __restrict__ part, const TR* __restrict__ R,
+                                                             TC* __restrict__ C, int M, int N, int S,
+                                                             const float* __restrict__ sa, const float* __restrict__ sw) {
+  const int ldc = EPI == 2 ? N / 2 : N;
+  const long n4 = (long)M * ldc / 4, mn = (long)M * N;
+  auto sums = [&](int row, int col, float (&v)[4]) {
+    const int* p = part + (long)row * N + col;
+    int4 a = *(const int4*)p;
+    for (int s = 1; s < S; ++s) {
+      const int4 b = *(const int4*)(p + s * mn);
+      a.x += b.x, a.y += b.y, a.z += b.z, a.w += b.w;
+    }
+    const float f = sa[row];
+    const float4 w = *(const float4*)(sw + col);
+    v[0] = (float)a.x * (f * w.x), v[1] = (float)a.y * (f * w.y), v[2] = (float)a.z * (f * w.z), v[3] = (float)a.w * (f * w.w);
+  };
+  for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n4; i += (long)gridDim.x * 256) {
+    const int row = (int)(i * 4 / ldc), j = (int)(i * 4 - (long)row * ldc);
+    float v[4];
+    if constexpr (EPI == 2) {
+      const int g = j / kGateUpBlock * (2 * kGateUpBlock) + j % kGateUpBlock;
+      float u[4];
+      sums(row, g, v);
+      sums(row, g + kGateUpBlock, u);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = silu_fast(v[e]) * u[e];
+    } else {
+      sums(row, j, v);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (EPI == 1) v[e] += ld_elt<TR>(R, i * 4 + e);
+    }
+    if constexpr (std::is_same<TC, float>::value) ((float4*)C)[i] = make_float4(v[0], v[1], v[2], v[3]);
+    else ((uint2*)C)[i] = make_uint2(pack_bf2(v[0], v[1]), pack_bf2(v[2], v[3]));
+  }
+}
+
+template <int MB, int WN, int EPI, typename TR, typename TC, bool DIRECT>
+int skinny_k(const Args& x, int S, int* part) {
+  constexpr size_t lds = skinny::lds_bytes<MB, WN>();
+  static const hipError_t attr =
+      hipFuncSetAttribute((const void*)gemm_skinny_kernel<int8_t, MB, WN, EPI, TR, TC, DIRECT>,
+                          hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  if (attr != hipSuccess) return -1;
+  hipLaunchKernelGGL((gemm_skinny_kernel<int8_t, MB, WN, EPI, TR, TC, DIRECT>), dim3(x.N / (64 * WN), S), dim3(skinny::NT),
+                     lds, x.st, (const bf16_t*)x.a, (const bf16_t*)x.w, part, (const TR*)x.r, (TC*)x.c, x.M, x.N, x.K, S,
+                     I8Scales{x.sa, x.sw});
+  return 0;
+}
+
+template <int MB, int EPI, typename TR, typename TC>
+int skinny_mb(const Args& x, SkinnyPlan pl, int* part) {
+  if (pl.wn == 4) return skinny_k<MB, 4, EPI, TR, TC, true>(x, 1, part);
+  if (pl.s == 1 && pl.wn == 2) return skinny_k<MB, 2, EPI, TR, TC, true>(x, 1, part);
+  if constexpr (EPI != 2) {
+    if (pl.s == 1) return skinny_k<MB, 1, EPI, TR, TC, true>(x, 1, part);
+  }
+  // the partial kernel does not depend on the epilogue's types, only (its weight rows) on SwiGLU with two blocks
+  if (pl.wn == 2 ? skinny_k<MB, 2, EPI == 2 ? 2 : 0, float, float, false>(x, pl.s, part)
+                 : skinny_k<MB, 1, 0, float, float, false>(x, pl.s, part))
+    return -1;
+  const long n4 = (long)x.M * (EPI == 2 ? x.N / 2 : x.N) / 4;
+  hipLaunchKernelGGL((gemm_i8_reduce_kernel<EPI, TR, TC>), dim3((int)std::min<long>((n4 + 255) / 256, 4096)), dim3(256), 0,
+                     x.st, part, (const TR*)x.r, (TC*)x.c, x.M, x.N, pl.s, x.sa, x.sw);
+  return 0;
+}
+
+template <int EPI, typename TR, typename TC>
+int launch_skinny(const Args& x, int* part) {
+  const SkinnyPlan pl = gemm_skinny_plan(x.M, x.N, pad(x.K, skinny::KS));
+  switch ((x.M + 15) / 16) {
+    case 1: return skinny_mb<1, EPI, TR, TC>(x, pl, part);
+    case 2: return skinny_mb<2, EPI, TR, TC>(x, pl, part);
+    case 3: return skinny_mb<3, EPI, TR, TC>(x, pl, part);
+    default: return skinny_mb<4, EPI, TR, TC>(x, pl, part);
+  }
+}
+
+}  // namespace
+
+int gemm_i8_check(int epi, int M, int N, int K) {
+  if (M < 0 || N <= 0 || K <= 0 || epi < 0 || epi > 2) return -1;
+  return N % 64 == 0 && K % 64 == 0 && K < (1 << 17) ? 0 : -1;
+}
+
+size_t gemm_i8_workspace_bytes(int M, int N, int K) {
+  if (M <= 0 || M > skinny::MAXM || gemm_i8_check(0, M, N, K)) return 0;
+  return (size_t)gemm_skinny_plan(M, N, pad(K / 2, skinny::KS)).s * M * N * sizeof(int);
+}
+
+int launch_gemm_i8(int r_dt, int c_dt, int epi, int M, int N, int K, const void* A, const float* a_scale, const void* W,
+                   const float* w_scale, const void* R, void* C, void* ws, size_t ws_bytes, hipStream_t st) {
+  if (M == 0) return 0;
+  if (gemm_i8_check(epi, M, N, K) || ws_bytes < gemm_i8_workspace_bytes(M, N, K)) return -1;
+  const Args x{M, N, K / 2, A, a_scale, W, w_scale, R, C, st};
+#define PS_I8_CASE(E, TR, TC, rd, cd) \
+  if (epi == E && (E != 1 || r_dt == rd) && c_dt == cd) \
+    return M <= skinny::MAXM ? launch_skinny<E, TR, TC>(x, (int*)ws) : launch_tiles<E, TR, TC>(x);
+  PS_I8_CASE(0, float, bf16_t, 0, 1)
+  PS_I8_CASE(0, float, float, 0, 0)
+  PS_I8_CASE(1, bf16_t, float, 1, 0)
+  PS_I8_CASE(1, float, bf16_t, 0, 1)
+  PS_I8_CASE(1, bf16_t, bf16_t, 1, 1)
+  PS_I8_CASE(1, float, float, 0, 0)
+  PS_I8_CASE(2, float, bf16_t, 0, 1)
+  PS_I8_CASE(2, float, float, 0, 0)
+#undef PS_I8_CASE
+  return -1;
+}
+
+}  // namespace ps

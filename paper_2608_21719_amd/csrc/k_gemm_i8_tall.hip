@@ -1,0 +1,6 @@
+// int8 tile GEMM instances: 256x128 and 192x128 tiles. The kernel is in gemm_tile.h.
+#include "gemm_tile.h"
+
+namespace ps {
+PS_I8_INSTANCES_TALL(PS_I8_INSTANTIATE)
+}  // namespace ps
