@@ -8,6 +8,7 @@ used for device memory and streams only (``data_ptr()``, ``cuda_stream``).
 Importing this module loads the library and raises ``LibraryMissing`` when it
 has not been built: there is no fallback path.
 """
+import array
 import ctypes
 import os
 from ctypes import POINTER, c_char_p, c_double, c_float, c_int32, c_size_t, c_uint64, c_void_p
@@ -184,31 +185,47 @@ def device_info(device: int = 0) -> dict:
 
 
 def ints(seq):
-    arr = (c_int32 * len(seq))(*[int(x) for x in seq])
-    return arr
+    """int32 array argument of a sequence of integers (64 of them 1.1 us; converted one by one 7)."""
+    try:
+        a = array.array("i", seq)
+    except TypeError:  # numbers that are not integers: truncated
+        a = array.array("i", [int(x) for x in seq])
+    return (c_int32 * len(a)).from_buffer(a) if a else (c_int32 * 0)()
 
 
 def ptr(t):
     """Device (or host) address of a torch tensor / numpy array / int / None."""
-    if t is None:
-        return None
-    if isinstance(t, int):
+    if t is None or isinstance(t, int):
         return t
-    if hasattr(t, "data_ptr"):
+    try:
         return t.data_ptr()
-    if hasattr(t, "ctypes"):
-        return t.ctypes.data
-    raise TypeError(type(t))
+    except AttributeError:
+        if hasattr(t, "ctypes"):
+            return t.ctypes.data
+        raise TypeError(type(t)) from None
 
 
 def stream_handle(stream=None):
     """The caller's HIP stream: an explicit handle, a torch stream, or torch's current stream."""
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        return _current_stream()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
+
+
+def _current_stream():
+    """Handle of torch's current stream on the current device, without a Stream object made for it where torch can
+    (0.3 us instead of 2)."""
+    global _current_stream
+    import torch
+    c = torch._C
+    if hasattr(c, "_cuda_getCurrentRawStream") and hasattr(c, "_cuda_getDevice"):
+        torch.cuda.init()
+        _current_stream = lambda: c._cuda_getCurrentRawStream(c._cuda_getDevice())  # noqa: E731
+    else:
+        _current_stream = lambda: torch.cuda.current_stream().cuda_stream  # noqa: E731
+    return _current_stream()
 
 
 def make_cfg(shape) -> LayerCfg:
@@ -340,11 +357,11 @@ class KV:
 
     def append(self, layer, seqs, n_tok, k, v, ws, stream=None):
         check(lib.ps_kv_append(self.h, layer, len(seqs), ints(seqs), ints(n_tok), ptr(k), ptr(v), ptr(ws),
-                               ws.numel() * ws.element_size(), stream_handle(stream)))
+                               ws.nbytes, stream_handle(stream)))
 
     def gather(self, layer, seq, k_out, v_out, ws, stream=None):
         check(lib.ps_kv_gather(self.h, layer, seq, ptr(k_out), ptr(v_out), ptr(ws),
-                               ws.numel() * ws.element_size(), stream_handle(stream)))
+                               ws.nbytes, stream_handle(stream)))
 
 
 class KV8(KV):
@@ -359,7 +376,7 @@ class KV8(KV):
 
 def kv_transfer(src: KV, src_seq: int, dst: KV, dst_seq: int, ws, stream=None):
     """Copy a sequence's KV state (every layer) from pool src to pool dst (think -> answer handoff)."""
-    check(lib.ps_kv_transfer(src.h, src_seq, dst.h, dst_seq, ptr(ws), ws.numel() * ws.element_size(),
+    check(lib.ps_kv_transfer(src.h, src_seq, dst.h, dst_seq, ptr(ws), ws.nbytes,
                              stream_handle(stream)))
 
 
@@ -493,16 +510,16 @@ class Layer:
 
     def prefill(self, w: LayerW, kv: KV, layer, seqs, n_tok, x_in, x_out, ws, stream=None):
         check(lib.ps_prefill(self.h, ctypes.byref(w), kv.h, layer, len(seqs), ints(seqs), ints(n_tok), ptr(x_in),
-                             ptr(x_out), ptr(ws), ws.numel() * ws.element_size(), stream_handle(stream)))
+                             ptr(x_out), ptr(ws), ws.nbytes, stream_handle(stream)))
 
     def decode_step(self, w: LayerW, kv: KV, layer, phase, seqs, x_in, x_out, ws, stream=None):
         check(lib.ps_decode_step(self.h, ctypes.byref(w), kv.h, layer, phase, len(seqs), ints(seqs), ptr(x_in),
-                                 ptr(x_out), ptr(ws), ws.numel() * ws.element_size(), stream_handle(stream)))
+                                 ptr(x_out), ptr(ws), ws.nbytes, stream_handle(stream)))
 
     def mixed_step(self, w: LayerW, kv: KV, layer, chunk_seqs, chunk_tok, dec_seqs, x_in, x_out, ws, stream=None):
         check(lib.ps_mixed_step(self.h, ctypes.byref(w), kv.h, layer, len(chunk_seqs), ints(chunk_seqs),
                                 ints(chunk_tok), len(dec_seqs), ints(dec_seqs), ptr(x_in), ptr(x_out), ptr(ws),
-                                ws.numel() * ws.element_size(), stream_handle(stream)))
+                                ws.nbytes, stream_handle(stream)))
 
     def step_plan(self, kv: KV, chunk_seqs, chunk_tok, dec_seqs, ws_bytes) -> StepPlan:
         out = StepPlan()
@@ -543,11 +560,11 @@ class Model:
 
     def prefill(self, kv: "KV", seqs, n_tok, tokens, next_tok, ws, logits=None, stream=None):
         check(lib.ps_model_prefill(self.h, kv.h, len(seqs), ints(seqs), ints(n_tok), ptr(tokens), ptr(next_tok),
-                                   ptr(logits), ptr(ws), ws.numel() * ws.element_size(), stream_handle(stream)))
+                                   ptr(logits), ptr(ws), ws.nbytes, stream_handle(stream)))
 
     def decode_step(self, kv: "KV", phase, seqs, tokens, next_tok, ws, logits=None, stream=None):
         check(lib.ps_model_decode_step(self.h, kv.h, phase, len(seqs), ints(seqs), ptr(tokens), ptr(next_tok),
-                                       ptr(logits), ptr(ws), ws.numel() * ws.element_size(), stream_handle(stream)))
+                                       ptr(logits), ptr(ws), ws.nbytes, stream_handle(stream)))
 
 
 def op_argmax(rows, vocab, logits, next_tok, stream=None):
@@ -568,7 +585,7 @@ def op_gemm_workspace_bytes(dtype, M, N, K) -> int:
 
 
 def op_gemm(dtype, r_dt, c_dt, epi, M, N, K, A, W, R, C, ws=None, stream=None):
-    wsb = 0 if ws is None else ws.numel() * ws.element_size()
+    wsb = 0 if ws is None else ws.nbytes
     check(lib.ps_op_gemm(dtype, r_dt, c_dt, epi, M, N, K, ptr(A), ptr(W), ptr(R), ptr(C), ptr(ws), wsb,
                          stream_handle(stream)))
 
@@ -592,36 +609,36 @@ def op_gemm_i8_workspace_bytes(M, N, K) -> int:
 
 
 def op_gemm_i8(r_dt, c_dt, epi, M, N, K, A, a_scale, W, w_scale, R, C, ws=None, stream=None):
-    wsb = 0 if ws is None else ws.numel() * ws.element_size()
+    wsb = 0 if ws is None else ws.nbytes
     check(lib.ps_op_gemm_i8(r_dt, c_dt, epi, M, N, K, ptr(A), ptr(a_scale), ptr(W), ptr(w_scale), ptr(R), ptr(C), ptr(ws),
                             wsb, stream_handle(stream)))
 
 
 def op_rope_kvwrite(kv: KV, layer, seqs, n_tok, qkv, q_out, ws, stream=None):
     check(lib.ps_op_rope_kvwrite(kv.h, layer, len(seqs), ints(seqs), ints(n_tok), ptr(qkv), ptr(q_out), ptr(ws),
-                                 ws.numel() * ws.element_size(), stream_handle(stream)))
+                                 ws.nbytes, stream_handle(stream)))
 
 
 def op_attention(kv: KV, layer, seqs, n_tok, q, o, ws, stream=None):
     check(lib.ps_op_attention(kv.h, layer, len(seqs), ints(seqs), ints(n_tok), ptr(q), ptr(o), ptr(ws),
-                              ws.numel() * ws.element_size(), stream_handle(stream)))
+                              ws.nbytes, stream_handle(stream)))
 
 
 def op_decode_attention(kv: KV, layer, seqs, q, o, ws, split_pages=0, stream=None):
     check(lib.ps_op_decode_attention(kv.h, layer, len(seqs), ints(seqs), ptr(q), ptr(o), split_pages, ptr(ws),
-                                     ws.numel() * ws.element_size(), stream_handle(stream)))
+                                     ws.nbytes, stream_handle(stream)))
 
 
 def op_decode_plan(kv: KV, seqs, ws, split_pages=0, stream=None):
-    check(lib.ps_op_decode_plan(kv.h, len(seqs), ints(seqs), split_pages, ptr(ws), ws.numel() * ws.element_size(),
+    check(lib.ps_op_decode_plan(kv.h, len(seqs), ints(seqs), split_pages, ptr(ws), ws.nbytes,
                                 stream_handle(stream)))
 
 
 def op_decode_run(kv: KV, layer, q, o, ws, stream=None):
-    check(lib.ps_op_decode_run(kv.h, layer, ptr(q), ptr(o), ptr(ws), ws.numel() * ws.element_size(),
+    check(lib.ps_op_decode_run(kv.h, layer, ptr(q), ptr(o), ptr(ws), ws.nbytes,
                                stream_handle(stream)))
 
 
 def op_decode_run_capped(kv: KV, layer, q, o, ws, max_workgroups, stream=None):
-    check(lib.ps_op_decode_run_capped(kv.h, layer, ptr(q), ptr(o), ptr(ws), ws.numel() * ws.element_size(),
+    check(lib.ps_op_decode_run_capped(kv.h, layer, ptr(q), ptr(o), ptr(ws), ws.nbytes,
                                       max_workgroups, stream_handle(stream)))

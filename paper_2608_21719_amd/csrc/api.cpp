@@ -209,8 +209,15 @@ struct DecodeAttnPlan {
   size_t o_si = 0, o_bt = 0, o_di = 0, o_pb = 0, o_pc = 0, off_po = 0, off_pml = 0;
 };
 
+static std::vector<double> rope_inv_freq(const ps_layer_cfg& c) {
+  std::vector<double> f(c.head_dim / 2);
+  for (int j = 0; j < c.head_dim / 2; ++j) f[j] = std::pow(c.rope_theta, -2.0 * j / c.head_dim);
+  return f;
+}
+
 struct ps_kv {
   ps_layer_cfg cfg;
+  std::vector<double> inv_freq;  // RoPE's, of cfg (computing it takes 2 us)
   int32_t n_layers;
   void* pool;
   size_t layer_elts;  // elements per layer
@@ -219,7 +226,7 @@ struct ps_kv {
   DecodeAttnPlan dplan;
   bool e4m3;  // 8-bit storage (kv8.h): blocks of all layers, then the scales
   ps_kv(const ps_layer_cfg& c, int32_t nl, int32_t np, int32_t ms, int32_t mp, void* p, uint64_t seed, bool e4m3_ = false)
-      : cfg(c), n_layers(nl), pool(p),
+      : cfg(c), inv_freq(rope_inv_freq(c)), n_layers(nl), pool(p),
         layer_elts((size_t)np * c.n_kv_heads * 2 * PS_PAGE_TOKENS * c.head_dim), meta(np, ms, mp, seed), e4m3(e4m3_) {}
   size_t layer_bytes() const { return layer_elts * (e4m3 ? 1 : elt_bytes(cfg.dtype)); }
   void* layer_base(int layer) const { return (char*)pool + (size_t)layer * layer_bytes(); }
@@ -504,13 +511,14 @@ ps_status plan_seqs(const ps_kv* kv, int n, const int32_t* seqs, const int32_t* 
   if (n < 0 || (n > 0 && !seqs)) return fail(PS_E_INVALID, "bad sequence list");
   if (fixed_n < 0 && n > 0 && !n_tok) return fail(PS_E_INVALID, "null n_tok");
   std::string e;
+  std::vector<bool> listed(kv->meta.max_seqs());
   for (int i = 0; i < n; ++i) {
     const int32_t s = seqs[i];
     const int32_t nn = fixed_n >= 0 ? fixed_n : n_tok[i];
     if (nn <= 0) return fail(PS_E_INVALID, "every sequence needs at least one new token");
     if (int rc = kv->meta.check_writable(s, nn, e)) return fail(rc, e);
-    for (int j = 0; j < i; ++j)
-      if (seqs[j] == s) return fail(PS_E_INVALID, "sequence listed twice in one call");
+    if (listed[s]) return fail(PS_E_INVALID, "sequence listed twice in one call");
+    listed[s] = true;
     const KvSeq& q = kv->meta.seq(s);
     SeqInfo inf;
     inf.kv_before = q.len;
@@ -763,6 +771,7 @@ std::vector<PrefillItem> plan_prefill(const std::vector<SeqInfo>& si, size_t cou
 struct PrefillSplit {
   std::vector<PrefillSplitItem> items;
   std::vector<PrefillMerge> merges;
+  std::vector<PrefillRange> ranges;  // of items, a workgroup each (plan_prefill_ranges)
   int32_t n_parts = 0;
 };
 
@@ -847,6 +856,91 @@ PrefillSplit plan_prefill_split(const std::vector<SeqInfo>& si, size_t count, in
   return P;
 }
 
+// The e4m3 kernel's split: the query tiles' walks laid end to end and cut into
+// equal ranges, one workgroup each (and KV head), so that every one ends at the
+// same time whatever the lengths; a range that ends inside a walk leaves a part.
+// For one, two and three workgroups per compute unit; the cheapest of them and
+// the whole walks is taken. Costs in us, measured: a key tile takes kTile[r] with r
+// workgroups on a unit, an item kItem beside its tiles, the merge as above. Whole
+// walks -> ranges, 8B heads: 64 rows behind 16000 tokens 353 -> 52, 512 behind 4000
+// 100 -> 68, 1024 behind 8000 211 -> 176, 445, 365 and 426 behind 7000 235 -> 179, 9
+// behind 1500 37 -> 22; 2048 behind 8000 (325) and more stay whole (3071 cut into
+// ranges 465 -> 517).
+template <typename MaxParts>
+PrefillSplit plan_prefill_ranges(const std::vector<SeqInfo>& si, size_t count, int groups, int n_q, MaxParts&& max_parts_of) {
+  PrefillSplit best;
+  const int qt = fa_query_tile(), kt = fa_key_tile();
+  constexpr double kTile[4] = {0, 0.72, 1.03, 1.55}, kItem = 3.0;
+  constexpr int kMin = 12;  // key tiles of an item that is cut
+  struct Tile {
+    int32_t b, q0, tiles;
+  };
+  std::vector<Tile> t;
+  const int slots = 3 * compute_units() / std::max(1, groups);
+  long total = 0;
+  int longest = 0;
+  for (size_t b = 0; b < count; ++b)
+    for (int32_t q0 = 0; q0 < si[b].n_new; q0 += qt) {
+      if ((int)t.size() >= slots) return best;
+      const int32_t keys = si[b].kv_before + std::min(q0 + qt, si[b].n_new);
+      t.push_back(Tile{(int32_t)b, q0, (keys + kt - 1) / kt});
+      total += t.back().tiles;
+      longest = std::max(longest, t.back().tiles);
+    }
+  if (longest < 2 * kMin) return best;
+  const int max_parts = max_parts_of();
+  const int fill = std::min(3, std::max(1, ((int)t.size() * groups + compute_units() - 1) / compute_units()));
+  // with three on a unit the longest walk runs beside shorter ones that end before it
+  const double walk = fill < 3 ? longest : 0.5 * (longest + (double)total / t.size());
+  double cost = 0.95 * (walk * kTile[fill] + kItem);  // a split has to promise a twentieth
+  for (int r = 1; r <= 3; ++r) {
+    const int n = r * compute_units() / std::max(1, groups);  // ranges
+    if (n < 1) continue;
+    long target = std::max<long>((total + n - 1) / n, kMin);
+    PrefillSplit p;
+    long load, most;  // key tiles of the open range, and of the fullest
+    int items, most_items;
+    for (;; target += std::max<long>(1, target / 32)) {  // until the ranges are n at most and the parts fit the room
+      p = PrefillSplit{};
+      load = most = 0, items = 0, most_items = 1;
+      auto close = [&] {
+        if (items == 0) return;
+        p.ranges.push_back(PrefillRange{(int32_t)p.items.size() - items, (int32_t)p.items.size()});
+        most = std::max(most, load);
+        most_items = std::max(most_items, items);
+        load = items = 0;
+      };
+      for (const Tile& x : t) {
+        const int32_t first = (int32_t)p.items.size();
+        for (int32_t at = 0; at < x.tiles;) {
+          long take = std::min<long>(x.tiles - at, target - load);
+          if (x.tiles - at - take < kMin) take = x.tiles - at;  // no short end
+          if (take < kMin && take < x.tiles - at) {              // nor a short beginning
+            close();
+            continue;
+          }
+          p.items.push_back(PrefillSplitItem{x.b, x.q0, at, (int32_t)(at + take), -1});
+          at += (int32_t)take;
+          load += take;
+          ++items;
+          if (load >= target) close();
+        }
+        const int32_t k = (int32_t)p.items.size() - first;
+        if (k == 1) continue;
+        p.merges.push_back(PrefillMerge{si[x.b].row_start + x.q0, std::min(qt, si[x.b].n_new - x.q0), p.n_parts, k});
+        for (int32_t i = 0; i < k; ++i) p.items[first + i].part = p.n_parts + i;
+        p.n_parts += k;
+      }
+      close();
+      if (p.n_parts == 0 || ((int)p.ranges.size() <= n && p.n_parts <= max_parts)) break;
+    }
+    if (p.n_parts == 0) continue;
+    const double c = most * kTile[r] + most_items * kItem + 8.0 + p.n_parts * (double)qt * n_q * 128 * 8.0 / 4.0e6;
+    if (c < cost) cost = c, best = std::move(p);
+  }
+  return best;
+}
+
 // Bytes of one part: O, and its bases and sums.
 size_t fa_part_bytes(int n_q) { return (size_t)fa_query_tile() * n_q * 128 * sizeof(float); }
 size_t fa_part_ml_bytes(int n_q) { return (size_t)fa_query_tile() * n_q * 2 * sizeof(float); }
@@ -858,12 +952,6 @@ bool fa_ok(const ps_layer_cfg& c) { return use_mfma_attn(c) && group_of(c) % 4 =
 bool dec_ok(const ps_layer_cfg& c) {
   const int g = group_of(c);
   return use_mfma_attn(c) && (g == 1 || g == 2 || g == 4 || g == 8 || g == 16);
-}
-
-std::vector<double> inv_freq(const ps_layer_cfg& c) {
-  std::vector<double> f(c.head_dim / 2);
-  for (int j = 0; j < c.head_dim / 2; ++j) f[j] = std::pow(c.rope_theta, -2.0 * j / c.head_dim);
-  return f;
 }
 
 // Bytes of a layer call's GEMM partials, on the caller's stream and on the
@@ -932,7 +1020,8 @@ size_t meta_bound(const ps_layer_cfg& c, int32_t max_rows, int32_t max_seqs, int
   const size_t parts = (size_t)max_seqs * ((max_pages + 7) / 8);
   b += align_up(sizeof(DecodeItem) * parts, 256) + 2 * align_up(4ull * max_seqs, 256);
   b += align_up(sizeof(PrefillItem) * ((size_t)max_rows / 32 + max_seqs), 256);
-  // split prefill items: at most one per workgroup slot
+  // split prefill items: at most one per workgroup slot (an e4m3 pool's list may be longer; without room
+  // for it the call takes the whole walks)
   if (fa_ok(c)) b += 2 * align_up(sizeof(PrefillSplitItem) * 3 * compute_units(), 256);
   return b + 256;
 }
@@ -958,6 +1047,42 @@ ps_status last_launch_error() {
 
 }  // namespace
 
+namespace {
+
+// The write into an e4m3 pool as one launch that carries its work list, where the
+// touched pages fit (a decode step, a few prompts): items > 0, else 0.
+int inline_write_items(const CallSeqs& cs, const ps_kv* kv, Kv8WriteMeta& m) {
+  int n = 0;
+  for (const SeqInfo& s : cs.si) {
+    const int32_t end = s.kv_before + s.n_new;
+    for (int32_t pos = s.kv_before; pos < end;) {
+      if (n == kKv8InlineItems) return 0;
+      const int32_t p = pos / PS_PAGE_TOKENS, stop = std::min(end, (p + 1) * PS_PAGE_TOKENS);
+      m.item[n++] = Kv8WriteItem{cs.bt[s.bt_off + p], pos, stop - pos, s.row_start + pos - s.kv_before};
+      pos = stop;
+    }
+  }
+  std::copy(kv->inv_freq.begin(), kv->inv_freq.end(), m.inv_freq);
+  return n;
+}
+
+// A small prefill call's work list as a kernel argument; false where it does not fit.
+bool inline_prefill(const CallSeqs& cs, const std::vector<PrefillItem>& items, Kv8PrefillMeta& m) {
+  if (cs.si.size() > Kv8PrefillMeta::kSeqs || items.size() > Kv8PrefillMeta::kItems || cs.bt.size() > Kv8PrefillMeta::kPages)
+    return false;
+  std::copy(cs.si.begin(), cs.si.end(), m.seq);
+  std::copy(items.begin(), items.end(), m.item);
+  std::copy(cs.bt.begin(), cs.bt.end(), m.page);
+  return true;
+}
+
+// Metadata bytes that the call's other form uploads to the workspace (asked for either way).
+size_t write_meta_bytes(const CallSeqs& cs, size_t freq_bytes) {
+  return align_up(align_up(align_up(cs.si.size() * sizeof(SeqInfo), 256) + cs.bt.size() * 4, 256) + freq_bytes, 256);
+}
+
+}  // namespace
+
 // ------------------------------------------------------------ KV device ops
 extern "C" ps_status ps_kv_append(ps_kv* kv, int32_t layer, int32_t n_seqs, const int32_t* seqs,
                                   const int32_t* n_tok, const void* k, const void* v, void* ws, size_t ws_bytes,
@@ -968,6 +1093,13 @@ extern "C" ps_status ps_kv_append(ps_kv* kv, int32_t layer, int32_t n_seqs, cons
   if (ps_status rc = plan_seqs(kv, n_seqs, seqs, n_tok, -1, cs)) return rc;
   if (cs.rows > 0 && (!k || !v)) return fail(PS_E_INVALID, "null k or v");
   if (ps_status rc = check_aligned({k, v})) return rc;
+  hipStream_t st = (hipStream_t)stream;
+  Kv8WriteMeta im;
+  if (const int n = kv->e4m3 ? inline_write_items(cs, kv, im) : 0) {
+    if (ps_status rc = check_ws(ws, ws_bytes, write_meta_bytes(cs, 0))) return rc;
+    launch_kv8_write_inline(im, n, false, k, v, nullptr, kv->layer8(layer), 0, kv->cfg.n_kv_heads, kv->cfg.head_dim, st);
+    return last_launch_error();
+  }
   Meta mt;
   const size_t o_si = mt.add(cs.si.data(), cs.si.size() * sizeof(SeqInfo));
   const size_t o_bt = mt.add(cs.bt.data(), cs.bt.size() * 4);
@@ -977,7 +1109,6 @@ extern "C" ps_status ps_kv_append(ps_kv* kv, int32_t layer, int32_t n_seqs, cons
   const int slot = kv->staging.acquire(mt.size(), &host);
   if (slot < 0) return PS_E_HIP;
   std::memcpy(host, mt.buf.data(), mt.buf.size());
-  hipStream_t st = (hipStream_t)stream;
   if (ps_status rc = kv->staging.submit(slot, ws, mt.buf.size(), st)) return rc;
   char* w = (char*)ws;
   if (kv->e4m3)
@@ -1265,7 +1396,8 @@ struct LayerPlan {
   size_t o_si = 0, o_bt = 0, o_fr = 0, o_pi = 0, o_di = 0, o_pb = 0, o_pc = 0;
   int n_pitems = 0, n_ditems = 0;
   int n_merges = 0;  // > 0: the prefill items are split ones
-  size_t o_mg = 0;
+  int n_ranges = 0;  // of an e4m3 pool's split items
+  size_t o_mg = 0, o_rg = 0;
   int32_t n_parts = 0;
   int32_t n_seqs = 0;
   Meta mt;
@@ -1298,23 +1430,25 @@ ps_status plan_layer(const ps_layer_cfg& c, const SplitGemms& split, const ps_kv
   P.gemm = gemm_room(c, split, P.rows);
   P.o_si = P.mt.add(cs.si.data(), cs.si.size() * sizeof(SeqInfo));
   P.o_bt = P.mt.add(cs.bt.data(), cs.bt.size() * 4);
-  const std::vector<double> fr = inv_freq(c);
-  P.o_fr = P.mt.add(fr.data(), fr.size() * 8);
+  P.o_fr = P.mt.add(kv->inv_freq.data(), kv->inv_freq.size() * 8);
   P.kv8 = kv->e4m3;
   P.fa = (P.kv8 || fa_ok(c)) && n_chunk > 0;
   P.dec_mfma = (P.kv8 || dec_ok(c)) && n_dec > 0;
   if (P.fa) {
     PrefillSplit sp;
-    if (may_split)
-      sp = plan_prefill_split(cs.si, n_chunk, fa_groups(c), c.n_q_heads, [&] {
-        P.fa_room = fa_layer_parts(c, P.chunk_rows, P.gemm);
-        return P.fa_room.parts;
-      });
+    auto room = [&] {
+      P.fa_room = fa_layer_parts(c, P.chunk_rows, P.gemm);
+      return P.fa_room.parts;
+    };
+    if (may_split && P.kv8) sp = plan_prefill_ranges(cs.si, n_chunk, fa_groups(c), c.n_q_heads, room);
+    else if (may_split) sp = plan_prefill_split(cs.si, n_chunk, fa_groups(c), c.n_q_heads, room);
     if (!sp.items.empty()) {
       P.n_pitems = (int)sp.items.size();
       P.n_merges = (int)sp.merges.size();
       P.o_pi = P.mt.add(sp.items.data(), sp.items.size() * sizeof(PrefillSplitItem));
       P.o_mg = P.mt.add(sp.merges.data(), sp.merges.size() * sizeof(PrefillMerge));
+      P.n_ranges = (int)sp.ranges.size();
+      P.o_rg = P.mt.add(sp.ranges.data(), sp.ranges.size() * sizeof(PrefillRange));
     } else {
       std::vector<PrefillItem> pitems = plan_prefill(cs.si, n_chunk);
       P.n_pitems = (int)pitems.size();
@@ -1486,8 +1620,8 @@ int launch_layer(const ps_layer_cfg& c, const LayerPlan& P, const ps_layer_w* w,
       const PrefillSplitItem* items = (const PrefillSplitItem*)(W + P.o_pi);
       const PrefillMerge* merges = (const PrefillMerge*)(W + P.o_mg);
       if (P.kv8)
-        bad |= launch_kv8_prefill_split(G, c.head_dim, P.n_pitems, P.n_merges, c.n_kv_heads, qr, pool8, si, bt, items, merges,
-                                        parts, o, scale_log2, s);
+        bad |= launch_kv8_prefill_split(G, c.head_dim, P.n_ranges, P.n_merges, c.n_kv_heads, qr, pool8, si, bt, items,
+                                        (const PrefillRange*)(W + P.o_rg), merges, parts, o, scale_log2, s);
       else
         bad |= launch_fa_prefill_split(G, P.n_pitems, P.n_merges, c.n_kv_heads, qr, pool, si, bt, items, merges, parts, o,
                                        scale_log2, s);
@@ -2025,21 +2159,26 @@ extern "C" ps_status ps_op_rope_kvwrite(ps_kv* kv, int32_t layer, int32_t n_seqs
   if (ps_status rc = plan_seqs(kv, n_seqs, seqs, n_tok, -1, cs)) return rc;
   if (cs.rows > 0 && (!qkv || !q_out)) return fail(PS_E_INVALID, "null pointer");
   if (ps_status rc = check_aligned({qkv, q_out})) return rc;
+  hipStream_t st = (hipStream_t)stream;
+  const ps_layer_cfg& c = kv->cfg;
+  Kv8WriteMeta im;
+  if (const int n = kv->e4m3 ? inline_write_items(cs, kv, im) : 0) {
+    if (ps_status rc = check_ws(ws, ws_bytes, write_meta_bytes(cs, kv->inv_freq.size() * 8))) return rc;
+    launch_kv8_write_inline(im, n, true, qkv, nullptr, q_out, kv->layer8(layer), c.n_q_heads, c.n_kv_heads, c.head_dim, st);
+    return last_launch_error();
+  }
   Meta mt;
   const size_t o_si = mt.add(cs.si.data(), cs.si.size() * sizeof(SeqInfo));
   const size_t o_bt = mt.add(cs.bt.data(), cs.bt.size() * 4);
-  const std::vector<double> fr = inv_freq(kv->cfg);
-  const size_t o_fr = mt.add(fr.data(), fr.size() * 8);
+  const size_t o_fr = mt.add(kv->inv_freq.data(), kv->inv_freq.size() * 8);
   if (ps_status rc = check_ws(ws, ws_bytes, mt.size())) return rc;
   if (cs.rows == 0) return PS_OK;
   void* host;
   const int slot = kv->staging.acquire(mt.size(), &host);
   if (slot < 0) return PS_E_HIP;
   std::memcpy(host, mt.buf.data(), mt.buf.size());
-  hipStream_t st = (hipStream_t)stream;
   if (ps_status rc = kv->staging.submit(slot, ws, mt.buf.size(), st)) return rc;
   char* W = (char*)ws;
-  const ps_layer_cfg& c = kv->cfg;
   if (kv->e4m3)
     launch_kv8_rope_write(cs.rows, qkv, q_out, kv->layer8(layer), (const SeqInfo*)(W + o_si), (const int32_t*)(W + o_bt),
                           (const double*)(W + o_fr), n_seqs, c.n_q_heads, c.n_kv_heads, c.head_dim, st);
@@ -2067,17 +2206,18 @@ extern "C" ps_status ps_op_attention(ps_kv* kv, int32_t layer, int32_t n_seqs, c
   const bool fa = kv->e4m3 || fa_ok(c);
   std::vector<PrefillItem> pitems;
   PrefillSplit sp;
-  size_t o_pi = 0, o_mg = 0, off_po = 0, off_ml = 0;
+  size_t o_pi = 0, o_mg = 0, o_rg = 0, off_po = 0, off_ml = 0;
   if (fa) {
     // split where the workspace has room for the partial results behind the metadata
     const size_t part = fa_part_bytes(c.n_q_heads), ml = fa_part_ml_bytes(c.n_q_heads);
-    const size_t fixed = mt.size() + 2 * align_up(sizeof(PrefillSplitItem) * 3 * compute_units(), 256) + 1024;
-    if (ws_bytes > fixed)
-      sp = plan_prefill_split(cs.si, cs.si.size(), fa_groups(c), c.n_q_heads,
-                              [&] { return (int)std::min<size_t>((ws_bytes - fixed) / (part + ml), 1 << 20); });
+    const size_t fixed = mt.size() + (kv->e4m3 ? 4 : 2) * align_up(sizeof(PrefillSplitItem) * 3 * compute_units(), 256) + 1024;
+    auto room = [&] { return (int)std::min<size_t>((ws_bytes - fixed) / (part + ml), 1 << 20); };
+    if (ws_bytes > fixed && kv->e4m3) sp = plan_prefill_ranges(cs.si, cs.si.size(), fa_groups(c), c.n_q_heads, room);
+    else if (ws_bytes > fixed) sp = plan_prefill_split(cs.si, cs.si.size(), fa_groups(c), c.n_q_heads, room);
     if (!sp.items.empty()) {
       o_pi = mt.add(sp.items.data(), sp.items.size() * sizeof(PrefillSplitItem));
       o_mg = mt.add(sp.merges.data(), sp.merges.size() * sizeof(PrefillMerge));
+      o_rg = mt.add(sp.ranges.data(), sp.ranges.size() * sizeof(PrefillRange));
       off_po = mt.size();
       off_ml = off_po + sp.n_parts * part;
       if (off_ml + sp.n_parts * ml > ws_bytes) return fail(PS_E_INVALID, "internal error: split attention workspace");
@@ -2088,6 +2228,14 @@ extern "C" ps_status ps_op_attention(ps_kv* kv, int32_t layer, int32_t n_seqs, c
   }
   if (ps_status rc = check_ws(ws, ws_bytes, mt.size())) return rc;
   if (cs.rows == 0) return PS_OK;
+  const float scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)c.head_dim));
+  Kv8PrefillMeta im;
+  if (kv->e4m3 && sp.items.empty() && inline_prefill(cs, pitems, im)) {
+    if (launch_kv8_prefill(group_of(c), c.head_dim, (int)pitems.size(), c.n_kv_heads, q, kv->layer8(layer), nullptr, nullptr,
+                           nullptr, o, scale_log2, (hipStream_t)stream, &im))
+      return fail(PS_E_UNSUPPORTED, "attention configuration not supported");
+    return last_launch_error();
+  }
   void* host;
   const int slot = kv->staging.acquire(mt.size(), &host);
   if (slot < 0) return PS_E_HIP;
@@ -2095,7 +2243,6 @@ extern "C" ps_status ps_op_attention(ps_kv* kv, int32_t layer, int32_t n_seqs, c
   hipStream_t st = (hipStream_t)stream;
   if (ps_status rc = kv->staging.submit(slot, ws, mt.buf.size(), st)) return rc;
   char* W = (char*)ws;
-  const float scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)c.head_dim));
   int bad;
   if (fa && !sp.items.empty()) {
     const FaPartials parts{{(float*)(W + off_po), nullptr, nullptr}, {sp.n_parts, sp.n_parts}, (float*)(W + off_ml)};
@@ -2105,8 +2252,9 @@ extern "C" ps_status ps_op_attention(ps_kv* kv, int32_t layer, int32_t n_seqs, c
     const PrefillMerge* merges = (const PrefillMerge*)(W + o_mg);
     const int n_items = (int)sp.items.size(), n_merges = (int)sp.merges.size();
     if (kv->e4m3)
-      bad = launch_kv8_prefill_split(group_of(c), c.head_dim, n_items, n_merges, c.n_kv_heads, q, kv->layer8(layer), si, bt,
-                                     items, merges, parts, o, scale_log2, st);
+      bad = launch_kv8_prefill_split(group_of(c), c.head_dim, (int)sp.ranges.size(), n_merges, c.n_kv_heads, q,
+                                     kv->layer8(layer), si, bt, items, (const PrefillRange*)(W + o_rg), merges, parts, o,
+                                     scale_log2, st);
     else
       bad = launch_fa_prefill_split(group_of(c), n_items, n_merges, c.n_kv_heads, q, kv->layer_base(layer), si, bt, items,
                                     merges, parts, o, scale_log2, st);

@@ -95,6 +95,12 @@ struct PrefillSplitItem {
   int32_t part;
 };
 
+// The consecutive items of one workgroup.
+struct PrefillRange {
+  int32_t begin;
+  int32_t end;
+};
+
 // A split query tile's merge: its first output row, rows, first part, parts.
 struct PrefillMerge {
   int32_t row;

@@ -223,42 +223,45 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   }
 }
 
-// o = sum_s o_s 2^(m_s - M) / sum_s l_s 2^(m_s - M), splits in order.
+// o = sum_s o_s 2^(m_s - M) / sum_s l_s 2^(m_s - M), splits in order: a workgroup
+// per (sequence, head). Its time is the latency of its loads, so every split's
+// statistics are read at once (a lane each) and the partials eight at a time.
 template <int HD>
 __global__ __launch_bounds__(HD) void kv8_combine_kernel(const float* __restrict__ part_o, const float* __restrict__ part_ml,
                                                          const int32_t* __restrict__ part_begin,
                                                          const int32_t* __restrict__ part_count, bf16_t* __restrict__ o,
                                                          int n_q) {
-  const int b = blockIdx.x, head = blockIdx.y, dim = threadIdx.x;
+  const int b = blockIdx.x, head = blockIdx.y, dim = threadIdx.x, lane = threadIdx.x & 63;
   const int np = part_count[b];
   if (np == 1) return;  // written by the attention kernel
   const long i0 = (long)part_begin[b] * n_q + head;  // part (p, head) is p n_q + head
-  float M = -INFINITY;
-  for (int i = 0; i < np; ++i) M = fmaxf(M, part_ml[(i0 + (long)i * n_q) * 2]);
-  float acc = 0.f, L = 0.f;
-  int i = 0;
-  for (; i + 4 <= np; i += 4) {  // four splits' loads overlap
-    float ov[4];
-    float2 ml[4];
+  float M = -INFINITY, L = 0.f, acc = 0.f;
+  // 64 splits at a time against a running maximum; each wave has the statistics in its lanes
+  for (int c0 = 0; c0 < np; c0 += 64) {
+    const int n = min(64, np - c0);
+    const long i = i0 + (long)c0 * n_q;
+    float2 ml = make_float2(-INFINITY, 0.f);
+    if (lane < n) ml = *(const float2*)(part_ml + (i + (long)lane * n_q) * 2);
+    float mx = ml.x;
+    for (int s = 32; s > 0; s >>= 1) mx = fmaxf(mx, __shfl_xor(mx, s));
+    mx = fmaxf(M, mx);
+    const float base = mx == -INFINITY ? 0.f : mx;  // only parts without a finite score yet: weights 0, not NaN
+    const float f = exp2f(ml.x - base), old = exp2f(M - base);
+    M = mx;
+    float l = ml.y * f;
+    for (int s = 32; s > 0; s >>= 1) l += __shfl_xor(l, s);
+    L = L * old + l;
+    acc *= old;
+    for (int k = 0; k < n; k += 8) {
+      float v[8];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const long pi = i0 + (long)(i + u) * n_q;
-      ov[u] = part_o[pi * HD + dim];
-      ml[u] = *(const float2*)(part_ml + pi * 2);
-    }
+      for (int u = 0; u < 8; ++u) v[u] = part_o[(i + (long)min(k + u, n - 1) * n_q) * HD + dim];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const float f = ml[u].x == -INFINITY ? 0.f : exp2f(ml[u].x - M);
-      acc += ov[u] * f;
-      L += ml[u].y * f;
+      for (int u = 0; u < 8; ++u) {
+        const float w = __shfl(f, (k + u) & 63);
+        acc += k + u < n ? v[u] * w : 0.f;
+      }
     }
-  }
-  for (; i < np; ++i) {
-    const long pi = i0 + (long)i * n_q;
-    const float2 ml = *(const float2*)(part_ml + pi * 2);
-    const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
-    acc += part_o[pi * HD + dim] * f;
-    L += ml.y * f;
   }
   o[((long)b * n_q + head) * HD + dim] = f2bf(acc / L);
 }
@@ -292,10 +295,11 @@ int launch_kv8_decode(int G, int hd, int n_items, int n_kv, int n_seqs, const vo
 // column of both and the statistics never cross lanes but between its halves.
 //
 // A tile's bytes go through registers: waves 0, 2 widen the keys of its pages,
-// waves 1, 3 the values, once for all four heads (16 conversions and four to
-// eight LDS stores per lane and tile), while the tile before it is multiplied;
-// the bytes themselves were requested another tile earlier. Masking of slots
-// without a token rides on the conversion.
+// waves 1, 3 the values, once for all four heads: 16 conversions and eight 8-byte
+// LDS stores per lane and tile, the same instructions for keys and values (only the
+// lane's LDS offsets differ), so that they run between the products of the tile
+// before. The bytes are requested two tiles before that, their page ids one more:
+// a walk alone on its compute unit waits for nothing but its own arithmetic.
 // LDS, two slots: K row = key, 16-byte chunk p of row r holds dims of chunk p ^
 // (r % 16) (hd 64: of 8 chunks, r % 8). V^T per page: row = dim, 16 tokens with
 // the quads in the order 0 2 1 3, which is how P lies in a lane (k = 8 g + e: token
@@ -311,29 +315,54 @@ __device__ __forceinline__ void kv8_lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-template <int HD, bool SPLIT>
+// Where the work list is: in memory, or (INLINE, small calls) the kernel's first
+// argument, which spares the call its upload (4 us of 17 for a prompt of 389).
+template <typename T>
+using Const = const __attribute__((address_space(4))) T*;  // kernel arguments
+struct NoPrefillMeta {};
+
+// SPLIT: a workgroup does the items of one range (PrefillRange), key ranges of
+// query tiles; parts leave O unnormalised with their base and sum for the merge.
+enum class Fa { kWhole, kInline, kSplit };
+template <int HD, Fa F>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void kv8_prefill_kernel(
-    const bf16_t* __restrict__ q, Kv8Layer kv, const SeqInfo* __restrict__ si, const int32_t* __restrict__ bt,
-    const typename std::conditional<SPLIT, PrefillSplitItem, PrefillItem>::type* __restrict__ items, bf16_t* __restrict__ o,
-    int n_kv, int G, float scale_log2, FaPartials parts) {
+    typename std::conditional<F == Fa::kInline, Kv8PrefillMeta, NoPrefillMeta>::type, const bf16_t* __restrict__ q, Kv8Layer kv,
+    const SeqInfo* __restrict__ si, const int32_t* __restrict__ bt,
+    const typename std::conditional<F == Fa::kSplit, PrefillSplitItem, PrefillItem>::type* __restrict__ items,
+    const PrefillRange* __restrict__ ranges, bf16_t* __restrict__ o, int n_kv, int G, float scale_log2, FaPartials parts) {
+  constexpr bool SPLIT = F == Fa::kSplit, INLINE = F == Fa::kInline;
   constexpr int KT = kPT, KK = HD / 16, DB = HD / 32, NB = HD / 64, CH = HD / 8;  // CH: 16-byte chunks of a K row
   constexpr int KE = kPageTokens * HD;  // elements of a page's keys
-  __shared__ __attribute__((aligned(1024))) bf16_t sK[2][KT * HD];
-  __shared__ __attribute__((aligned(1024))) bf16_t sV[2][KT * HD];
+  constexpr int TILE = KT * HD * 2;  // bytes of a tile's keys; its values follow
+  __shared__ __attribute__((aligned(1024))) char s_kv[2][2 * TILE];
   const int hq = (G + 3) / 4;
   const int kvh = blockIdx.y / hq;
-  const auto it = items[blockIdx.x];
-  const SeqInfo s = si[it.b];
   const int n_q = n_kv * G;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int g = lane >> 5, c = lane & 31;
   const int hi = (blockIdx.y % hq) * 4 + wave;
+  const auto* meta = (Const<Kv8PrefillMeta>)__builtin_amdgcn_kernarg_segment_ptr();
+  int i0 = blockIdx.x, i1 = i0 + 1;
+  if constexpr (SPLIT) i0 = ranges[blockIdx.x].begin, i1 = ranges[blockIdx.x].end;
+  for (int item = i0; item < i1; ++item) {
+  typename std::conditional<SPLIT, PrefillSplitItem, PrefillItem>::type it;
+  SeqInfo s;
+  typename std::conditional<INLINE, Const<int32_t>, const int32_t*>::type btr;
+  if constexpr (INLINE) {
+    it.b = meta->item[item].b, it.q_begin = meta->item[item].q_begin;
+    s.kv_before = meta->seq[it.b].kv_before, s.n_new = meta->seq[it.b].n_new;
+    s.row_start = meta->seq[it.b].row_start;
+    btr = meta->page + meta->seq[it.b].bt_off;
+  } else {
+    it = items[item];
+    s = si[it.b];
+    btr = bt + s.bt_off;
+  }
   const bool live = hi < G;
   const int head = kvh * G + min(hi, G - 1);
   const int qn = min(kPT, s.n_new - it.q_begin);
   const int qpos0 = s.kv_before + it.q_begin;
   const int kv_valid = s.kv_before + s.n_new;
-  const int32_t* btr = bt + s.bt_off;
   int kt0 = 0, n_tiles = (qpos0 + qn + KT - 1) / KT;
   if constexpr (SPLIT) kt0 = it.kt_begin, n_tiles = it.kt_end;
   const float2* scales = kv.scales + (long)kvh * kv.n_pages;
@@ -341,52 +370,45 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k
   // this wave's half of one page of a tile
   const int pg = wave >> 1;
   const bool values = wave & 1;
+  const int lq = lane >> 4, lc = lane & 15;
+  const int last_page = (kv_valid - 1) / kPageTokens;
   struct Raw {
     uint4 w[NB];
     float s;
-    int valid;  // tokens of the page that are written
   };
-  auto fetch = [&](int kt) __attribute__((always_inline)) {
+  // page ids are read ahead of the bytes; past the last page the last is read again, and masked
+  auto page_id = [&](int kt) __attribute__((always_inline)) { return btr[min(2 * kt + pg, last_page)]; };
+  auto fetch = [&](int page) __attribute__((always_inline)) {
     Raw r;
-    const int p = 2 * kt + pg;
-    r.valid = kv_valid - p * kPageTokens;
-    r.s = 0.f;
+    const uint8_t* base = kv.blocks + kv8_block(page, kvh, n_kv, HD) + (values ? KE : 0) + lane * 16;
+    r.s = values ? scales[page].y : scales[page].x;
 #pragma unroll
-    for (int i = 0; i < NB; ++i) r.w[i] = make_uint4(0, 0, 0, 0);
-    if (r.valid > 0) {
-      const int page = btr[p];
-      const uint8_t* base = kv.blocks + kv8_block(page, kvh, n_kv, HD) + (values ? KE : 0) + lane * 16;
-      const float2 sc = scales[page];
-      r.s = values ? sc.y : sc.x;
-#pragma unroll
-      for (int i = 0; i < NB; ++i) r.w[i] = *(const uint4*)(base + 1024 * i);
-    }
+    for (int i = 0; i < NB; ++i) r.w[i] = *(const uint4*)(base + 1024 * i);
     return r;
   };
-  const int lq = lane >> 4, lc = lane & 15;
-  auto put = [&](const Raw& r, int slot) __attribute__((always_inline)) {
-    if (!values) {  // lane: token lc, dims 64 i + 16 lq ..
-      char* row = (char*)sK[slot] + (16 * pg + lc) * HD * 2;
+  // LDS offset of the lane's word (i, j): keys: token lc, dims 64 i + 16 lq + 4 j ..; values: tokens 4 lq .., dim 64 i + 16 j + lc
+  int at[NB][4];
 #pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        const int ch = 8 * i + 2 * lq;
-        *(bf16x8_t*)(row + ((ch ^ (lc & (CH - 1))) << 4)) = e4m3_bf8(r.w[i].x, r.w[i].y, r.s);
-        *(bf16x8_t*)(row + (((ch + 1) ^ (lc & (CH - 1))) << 4)) = e4m3_bf8(r.w[i].z, r.w[i].w, r.s);
-      }
-    } else {  // lane: tokens 4 lq .., dims 64 i + 16 b + lc
-      const uint32_t keep = token_bytes(r.valid - 4 * lq);
-      char* page = (char*)sV[slot] + pg * KE * 2;
+  for (int i = 0; i < NB; ++i)
 #pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        const uint32_t w[4] = {r.w[i].x, r.w[i].y, r.w[i].z, r.w[i].w};
+    for (int j = 0; j < 4; ++j) {
+      const int ch = 8 * i + 2 * lq + (j >> 1), dim = 64 * i + 16 * j + lc;
+      at[i][j] = values ? TILE + pg * KE * 2 + dim * 32 + (((lq & 1) ^ ((dim >> 3) & 1)) << 4) + ((lq >> 1) << 3)
+                        : (16 * pg + lc) * HD * 2 + ((ch ^ (lc & (CH - 1))) << 4) + ((j & 1) << 3);
+    }
+  auto put = [&](Raw r, int kt, char* slot) __attribute__((always_inline)) {
+    const int valid = kv_valid - (2 * kt + pg) * kPageTokens;
+    if (valid < kPageTokens && values) {  // slots that hold no token may hold any byte: zero, so that 0 x NaN does not arise
+      const uint32_t keep = token_bytes(valid - 4 * lq);
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          const int dim = 64 * i + 16 * b + lc;
-          const uint32_t x = w[b] & keep;
-          *(uint2*)(page + dim * 32 + (((lq & 1) ^ ((dim >> 3) & 1)) << 4) + ((lq >> 1) << 3)) =
-              make_uint2(e4m3_bf2<false>(x, r.s), e4m3_bf2<true>(x, r.s));
-        }
-      }
+      for (int i = 0; i < NB; ++i) r.w[i] = make_uint4(r.w[i].x & keep, r.w[i].y & keep, r.w[i].z & keep, r.w[i].w & keep);
+    }
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      const uint32_t w[4] = {r.w[i].x, r.w[i].y, r.w[i].z, r.w[i].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *(uint2*)(slot + at[i][j]) = make_uint2(e4m3_bf2<false>(w[j], r.s), e4m3_bf2<true>(w[j], r.s));
     }
   };
 
@@ -408,19 +430,24 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k
   const uint32_t vread = (uint32_t)(c * 32 + ((g ^ ((c >> 3) & 1)) << 4));
   const int qpos = qpos0 + min(c, qn - 1);  // padding columns take the last row's keys
 
-  Raw next = fetch(kt0);
-  put(next, 0);
-  if (kt0 + 1 < n_tiles) next = fetch(kt0 + 1);
+  // tiles kt0 + t: bytes in raw[t & 1], then in LDS slot t & 1
+  Raw raw[2];
+  int id = page_id(kt0 + 2);
+  raw[0] = fetch(page_id(kt0));
+  raw[1] = fetch(page_id(kt0 + 1));
+  put(raw[0], kt0, s_kv[0]);
+  raw[0] = fetch(id);
+  id = page_id(kt0 + 3);
   kv8_lds_barrier();
 
-  auto tile = [&](int kt, int slot, auto firstc) __attribute__((always_inline)) {
+  auto tile = [&](int kt, auto slotc, auto firstc) __attribute__((always_inline)) {
     constexpr bool FIRST = decltype(firstc)::value;
+    constexpr int SLOT = decltype(slotc)::value;
     const int k0 = kt * KT;
-    const char *K = (const char*)sK[slot], *V = (const char*)sV[slot];
-    if (kt + 1 < n_tiles) {
-      put(next, slot ^ 1);
-      if (kt + 2 < n_tiles) next = fetch(kt + 2);
-    }
+    const char *K = s_kv[SLOT], *V = s_kv[SLOT] + TILE;
+    put(raw[SLOT ^ 1], kt + 1, s_kv[SLOT ^ 1]);  // past the walk's end: never read
+    raw[SLOT ^ 1] = fetch(id);
+    id = page_id(kt + 4);
     f32x16_t sacc;
 #pragma unroll
     for (int r = 0; r < 16; ++r) sacc[r] = 0.f;
@@ -493,12 +520,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k
     }
     kv8_lds_barrier();  // the next tile is written; every wave is done with this one
   };
-  tile(kt0, 0, std::true_type{});
-  for (int kt = kt0 + 1; kt < n_tiles; ++kt) tile(kt, (kt - kt0) & 1, std::false_type{});
+  using Even = std::integral_constant<int, 0>;
+  using Odd = std::integral_constant<int, 1>;
+  tile(kt0, Even{}, std::true_type{});
+  for (int kt = kt0 + 1; kt < n_tiles; kt += 2) {
+    tile(kt, Odd{}, std::false_type{});
+    if (kt + 1 < n_tiles) tile(kt + 1, Even{}, std::false_type{});
+  }
 
   const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(lsum), __float_as_uint(lsum), false, false);
   const float l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-  if (!live || c >= qn) return;
+  if (!live || c >= qn) continue;
   if constexpr (SPLIT) {
     if (it.part >= 0) {
       float* po = parts.part(it.part, (long)n_q * kPT * HD) + ((long)head * kPT + c) * HD;
@@ -509,7 +541,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k
           *(float4*)(po + 32 * db + 8 * rb + 4 * g) =
               make_float4(oacc[db][4 * rb], oacc[db][4 * rb + 1], oacc[db][4 * rb + 2], oacc[db][4 * rb + 3]);
       if (g == 0) *(float2*)(parts.ml + (((long)it.part * n_q + head) * kPT + c) * 2) = make_float2(mb, l);
-      return;
+      continue;
     }
   }
   const float inv = 1.f / l;
@@ -521,6 +553,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k
       *(uint2*)(op + 32 * db + 8 * rb + 4 * g) =
           make_uint2(pack_bf2(oacc[db][4 * rb] * inv, oacc[db][4 * rb + 1] * inv),
                      pack_bf2(oacc[db][4 * rb + 2] * inv, oacc[db][4 * rb + 3] * inv));
+  }
 }
 
 // Parts of a split query tile, in key order; a wave per head and row.
@@ -550,11 +583,19 @@ __global__ __launch_bounds__(256) void kv8_merge_kernel(const PrefillMerge* __re
 }
 
 int launch_kv8_prefill(int G, int hd, int n_items, int n_kv, const void* q, const Kv8Layer& kv, const SeqInfo* si,
-                       const int32_t* bt, const PrefillItem* items, void* o, float scale_log2, hipStream_t st) {
+                       const int32_t* bt, const PrefillItem* items, void* o, float scale_log2, hipStream_t st,
+                       const Kv8PrefillMeta* meta) {
   if (n_items == 0) return 0;
+  const dim3 grid(n_items, n_kv * ((G + 3) / 4));
   auto go = [&](auto hc) {
-    hipLaunchKernelGGL((kv8_prefill_kernel<decltype(hc)::value, false>), dim3(n_items, n_kv * ((G + 3) / 4)), dim3(256), 0, st,
-                       (const bf16_t*)q, kv, si, bt, items, (bf16_t*)o, n_kv, G, scale_log2, FaPartials{});
+    constexpr int HD = decltype(hc)::value;
+    if (meta)
+      hipLaunchKernelGGL((kv8_prefill_kernel<HD, Fa::kInline>), grid, dim3(256), 0, st, *meta, (const bf16_t*)q, kv,
+                         (const SeqInfo*)nullptr, (const int32_t*)nullptr, (const PrefillItem*)nullptr,
+                         (const PrefillRange*)nullptr, (bf16_t*)o, n_kv, G, scale_log2, FaPartials{});
+    else
+      hipLaunchKernelGGL((kv8_prefill_kernel<HD, Fa::kWhole>), grid, dim3(256), 0, st, NoPrefillMeta{}, (const bf16_t*)q, kv, si,
+                         bt, items, (const PrefillRange*)nullptr, (bf16_t*)o, n_kv, G, scale_log2, FaPartials{});
     return 0;
   };
   if (hd == 128) return go(std::integral_constant<int, 128>{});
@@ -562,15 +603,15 @@ int launch_kv8_prefill(int G, int hd, int n_items, int n_kv, const void* q, cons
   return -1;
 }
 
-int launch_kv8_prefill_split(int G, int hd, int n_items, int n_merges, int n_kv, const void* q, const Kv8Layer& kv,
-                             const SeqInfo* si, const int32_t* bt, const PrefillSplitItem* items, const PrefillMerge* merges,
-                             FaPartials part, void* o, float scale_log2, hipStream_t st) {
-  if (n_items == 0) return 0;
+int launch_kv8_prefill_split(int G, int hd, int n_ranges, int n_merges, int n_kv, const void* q, const Kv8Layer& kv,
+                             const SeqInfo* si, const int32_t* bt, const PrefillSplitItem* items, const PrefillRange* ranges,
+                             const PrefillMerge* merges, FaPartials part, void* o, float scale_log2, hipStream_t st) {
+  if (n_ranges == 0) return 0;
   const int n_q = n_kv * G;
   auto go = [&](auto hc) {
     constexpr int HD = decltype(hc)::value;
-    hipLaunchKernelGGL((kv8_prefill_kernel<HD, true>), dim3(n_items, n_kv * ((G + 3) / 4)), dim3(256), 0, st,
-                       (const bf16_t*)q, kv, si, bt, items, (bf16_t*)o, n_kv, G, scale_log2, part);
+    hipLaunchKernelGGL((kv8_prefill_kernel<HD, Fa::kSplit>), dim3(n_ranges, n_kv * ((G + 3) / 4)), dim3(256), 0, st,
+                       NoPrefillMeta{}, (const bf16_t*)q, kv, si, bt, items, ranges, (bf16_t*)o, n_kv, G, scale_log2, part);
     if (n_merges > 0)
       hipLaunchKernelGGL(kv8_merge_kernel<HD>, dim3(n_merges * kPT, (n_q + 3) / 4), dim3(256), 0, st, merges, part, (bf16_t*)o,
                          n_q);

@@ -98,6 +98,19 @@ int launch_fa_prefill(int G, int n_items, int n_kv, const void* q, const void* p
 int launch_kv8_rope_write(int rows, const void* qkv, void* q_out, const Kv8Layer& kv, const SeqInfo* si, const int32_t* bt,
                           const double* inv_freq, int n_seqs, int n_q, int n_kv, int hd, hipStream_t st,
                           const float* part = nullptr, int splits = 1);
+// The same write (or append: rope false, k and v) of few pages, its work list
+// passed as a kernel argument.
+struct Kv8WriteItem {
+  int32_t page, pos, n, row;  // tokens pos .. pos + n of one page, from row `row`
+};
+constexpr int kKv8InlineItems = 128;
+struct Kv8WriteMeta {
+  double inv_freq[64];
+  Kv8WriteItem item[kKv8InlineItems];
+};
+static_assert(sizeof(Kv8WriteMeta) <= 3584, "kernel arguments hold 4 KiB");
+int launch_kv8_write_inline(const Kv8WriteMeta& meta, int n_items, bool rope, const void* k, const void* v, void* q_out,
+                            const Kv8Layer& kv, int n_q, int n_kv, int hd, hipStream_t st);
 int launch_kv8_append(int rows, const void* k, const void* v, const Kv8Layer& kv, const SeqInfo* si, const int32_t* bt,
                       int n_seqs, int n_kv, int hd, hipStream_t st);
 int launch_kv8_gather(int len, const Kv8Layer& kv, const int32_t* bt, void* k_out, void* v_out, int n_kv, int hd,
@@ -110,12 +123,22 @@ int launch_kv8_decode(int G, int hd, int n_items, int n_kv, int n_seqs, const vo
                       const int32_t* bt, const DecodeItem* items, float* part_o, float* part_ml, const int32_t* part_begin,
                       const int32_t* part_count, void* o, float scale_log2, hipStream_t st, int max_wg = 0);
 // Prefill rows, any group size; work lists and partials as launch_fa_prefill and
-// launch_fa_prefill_split (the same query and key tiles).
+// launch_fa_prefill_split (the same query and key tiles), but a workgroup of the
+// split launch does a range of items one after the other. meta: the work list of
+// a small call, in place of si, bt and items.
+struct Kv8PrefillMeta {
+  static constexpr int kSeqs = 16, kItems = 128, kPages = 384;
+  SeqInfo seq[kSeqs];
+  PrefillItem item[kItems];
+  int32_t page[kPages];
+};
+static_assert(sizeof(Kv8PrefillMeta) <= 3584, "kernel arguments hold 4 KiB");
 int launch_kv8_prefill(int G, int hd, int n_items, int n_kv, const void* q, const Kv8Layer& kv, const SeqInfo* si,
-                       const int32_t* bt, const PrefillItem* items, void* o, float scale_log2, hipStream_t st);
-int launch_kv8_prefill_split(int G, int hd, int n_items, int n_merges, int n_kv, const void* q, const Kv8Layer& kv,
-                             const SeqInfo* si, const int32_t* bt, const PrefillSplitItem* items, const PrefillMerge* merges,
-                             FaPartials part, void* o, float scale_log2, hipStream_t st);
+                       const int32_t* bt, const PrefillItem* items, void* o, float scale_log2, hipStream_t st,
+                       const Kv8PrefillMeta* meta = nullptr);
+int launch_kv8_prefill_split(int G, int hd, int n_ranges, int n_merges, int n_kv, const void* q, const Kv8Layer& kv,
+                             const SeqInfo* si, const int32_t* bt, const PrefillSplitItem* items, const PrefillRange* ranges,
+                             const PrefillMerge* merges, FaPartials part, void* o, float scale_log2, hipStream_t st);
 
 // GEMM C = epi(A W^T); ws holds split-K partials for decode-sized M.
 // beside: another stream's kernels hold part of the chip, so a tile launch is
