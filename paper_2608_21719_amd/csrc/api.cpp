@@ -569,6 +569,26 @@ class DecodeCost {
            (rope_ && rounds > 1.0 ? 8.0 : 0.0);
   }
 
+  // The same for an e4m3 pool (n_kv here: workgroups per work item): 0.146 for each
+  // 4 KiB page of a unit's even share (28 GB/s), 0.075 for each that the fullest unit
+  // has beyond it (the others leave it bandwidth when they end), 1.0 for a round,
+  // and where a sequence is split 2.4, 0.03 for each split of the longest and 0.55
+  // for each MB of partial results both ways. Fitted over 3700 batches of 1 to 160
+  // sequences of 16 to 20000 tokens, 1 to 16 KV heads, head sizes of 64 and 128 (rms
+  // error 7%): the cheapest by this of the splits compared is 0.7% above the fastest
+  // of them on average, 5% at the 95th percentile (the 16-bit rule 5% and 26%: bytes
+  // pass twice as fast, so a split's own cost weighs twice as much).
+  double us8(long split, int n_q, int hd) {
+    const long items = cut(split);
+    long total = 0;
+    for (long p : pages_) total += p;
+    const double rounds = (double)items * n_kv_ / (2.0 * compute_units());
+    const double mean = (double)total / std::max(1, compute_units() / std::max(1, n_kv_));
+    const double parts = (double)items * n_q * hd * 8.0 / 1e6;
+    return (0.146 * mean + 0.075 * (fullest_unit_pages() - mean)) * (hd / 128.0) + 1.0 * rounds +
+           (most_splits_ > 1 ? 2.4 + 0.03 * most_splits_ + 0.55 * parts : 0.0);
+  }
+
  private:
   struct Run {  // `n` work items or compute units' shares, of `pages` pages each
     long pages, n;
@@ -725,6 +745,44 @@ int32_t choose_split_pages(const std::vector<SeqInfo>& si, size_t first, int n_k
   // rejected by the launcher)
   while (n_items(sp) > kMaxDecodeItems && sp < (1L << 24)) sp *= 2;
   return (int32_t)sp;
+}
+
+// For an e4m3 pool: of 8, 16, 32 .. pages and whole sequences the cheapest
+// (DecodeCost::us8), then of the lengths half-way to its neighbours.
+int32_t choose_split_pages8(const std::vector<SeqInfo>& si, size_t first, const ps_layer_cfg& c) {
+  std::vector<long> pages;
+  pages.reserve(si.size() - first);
+  long max_pages = 1;
+  for (size_t b = first; b < si.size(); ++b) {
+    pages.push_back((si[b].kv_before + si[b].n_new + 15) / 16);
+    max_pages = std::max(max_pages, pages.back());
+  }
+  const int wgs = c.n_kv_heads * ((c.n_q_heads / c.n_kv_heads + 15) / 16);
+  DecodeCost cost(pages, wgs, false);
+  auto n_items = [&](long spl) {
+    long n = 0;
+    for (long p : pages) n += (p + spl - 1) / spl;
+    return n;
+  };
+  const long most = std::min<long>(kMaxDecodeItems, std::max<long>((long)pages.size(), 16L * compute_units() / std::max(1, wgs)));
+  long best = max_pages;
+  double best_us = -1.0;
+  auto weigh = [&](long spl) {
+    if (spl < 8 || spl >= max_pages || n_items(spl) > most) return;  // whole sequences stand in for longer ones
+    const double us = cost.us8(spl, c.n_q_heads, c.head_dim);
+    if (us < best_us) best_us = us, best = spl;
+  };
+  if (max_pages <= 8) return (int32_t)max_pages;
+  best_us = cost.us8(max_pages, c.n_q_heads, c.head_dim);
+  for (long spl = 8; spl < max_pages && spl <= 256; spl *= 2) weigh(spl);
+  const long mid = best;
+  if (mid < max_pages) {
+    weigh(mid * 3 / 4);
+    weigh(mid * 3 / 2);
+  } else {
+    weigh(384);
+  }
+  return (int32_t)best;
 }
 
 DecodePlan plan_decode(const std::vector<SeqInfo>& si, size_t first, int32_t split_pages) {
@@ -1456,7 +1514,8 @@ ps_status plan_layer(const ps_layer_cfg& c, const SplitGemms& split, const ps_kv
     }
   }
   if (P.dec_mfma) {
-    DecodePlan dp = plan_decode(cs.si, n_chunk, choose_split_pages(cs.si, n_chunk, c.n_kv_heads, n_chunk == 0 && !P.kv8));
+    DecodePlan dp = plan_decode(cs.si, n_chunk, P.kv8 ? choose_split_pages8(cs.si, n_chunk, c)
+                                                      : choose_split_pages(cs.si, n_chunk, c.n_kv_heads, n_chunk == 0));
     if ((long)dp.items.size() > kMaxDecodeItems)
       return fail(PS_E_UNSUPPORTED, "decode batch exceeds 65535 attention work items");
     P.n_ditems = (int)dp.items.size();
@@ -2288,7 +2347,9 @@ extern "C" ps_status ps_op_decode_plan(ps_kv* kv, int32_t n_seqs, const int32_t*
   DecodeAttnPlan pl;
   pl.o_si = mt.add(cs.si.data(), cs.si.size() * sizeof(SeqInfo));
   pl.o_bt = mt.add(cs.bt.data(), cs.bt.size() * 4);
-  const int32_t sp = split_pages > 0 ? split_pages : choose_split_pages(cs.si, 0, c.n_kv_heads, false);
+  const int32_t sp = split_pages > 0 ? split_pages
+                     : kv->e4m3      ? choose_split_pages8(cs.si, 0, c)
+                                     : choose_split_pages(cs.si, 0, c.n_kv_heads, false);
   DecodePlan dp = plan_decode(cs.si, 0, sp);
   if ((long)dp.items.size() > kMaxDecodeItems)
     return fail(PS_E_UNSUPPORTED, "more than 65535 attention work items: use larger split_pages");
