@@ -543,8 +543,9 @@ ps_status ps_op_tile_weight_i8(int32_t N, int32_t K, const void* w, void* out, v
  * ps_op_gemm (SwiGLU: W rows and w_scale in w_gate_up's order; r_dtype is read
  * for PS_EPI_RESIDUAL only). c_dtype PS_F32 or PS_BF16; R of r_dtype may alias C
  * when the dtypes match. N and K multiples of 64, K < 131072 (the sums then fit),
- * any M; M <= 64 needs ws of ps_op_gemm_i8_workspace_bytes (0 bytes otherwise). The
- * result does not depend on how the product is cut up: calls repeat bit for bit. */
+ * any M; ws of ps_op_gemm_i8_workspace_bytes (which may be 0) holds the partial
+ * sums of products split over K. The result does not depend on how the product is
+ * cut up: calls repeat bit for bit. */
 size_t ps_op_gemm_i8_workspace_bytes(int32_t M, int32_t N, int32_t K);
 ps_status ps_op_gemm_i8(int32_t r_dtype, int32_t c_dtype, int32_t epilogue, int32_t M, int32_t N, int32_t K, const void* A,
                         const float* a_scale, const void* W, const float* w_scale, const void* R, void* C, void* ws,

@@ -206,7 +206,8 @@ constexpr int share(int n, int mf, int q) { return n * q / mf; }
 
 // K in 16-bit units. int8 operands (Operand<int8_t>): N a multiple of 64 that
 // need not fill the last tile, K one of 32 units (W's tiles are padded with
-// zeros, whatever A's next row or the end of the buffer gives beside them).
+// zeros, whatever A's next row or the end of the buffer gives beside them). TC
+// int: a K split's int32 sums as they are (EPI 0).
 template <typename TE, int QM, int QN, int NS, bool NT, int EPI, typename TR, typename TC>
 __global__ __launch_bounds__(256) void gemm_tile_kernel(const bf16_t* __restrict__ A, const bf16_t* __restrict__ W,
                                                         const TR* __restrict__ R, TC* __restrict__ C, int M, int N,
@@ -214,7 +215,7 @@ __global__ __launch_bounds__(256) void gemm_tile_kernel(const bf16_t* __restrict
                                                         typename Operand<TE>::Scales sc) {
   using namespace tile;
   using Op = Operand<TE>;
-  constexpr bool I8 = Op::kInt8;
+  constexpr bool I8 = Op::kInt8, RAW = std::is_same<TC, int>::value;
   const int KT = I8 ? (K + BK - 1) / BK : K / 64;  // W tiles along K
   using G = Geo<QM, QN, NS>;
   constexpr int BM = G::BM, BN = G::BN, STAGE = G::STAGE, A_LOADS = G::A_LOADS, B_LOADS = G::B_LOADS, LOADS = G::LOADS;
@@ -440,12 +441,12 @@ __global__ __launch_bounds__(256) void gemm_tile_kernel(const bf16_t* __restrict
   // and, a block ahead like the residual, its rows' scales
   float swv[I8 ? (EPI == 2 ? 2 : 1) : 1][I8 ? V : 1], sav[2][I8 ? NPASS : 1];
   auto load_sa = [&](int i) __attribute__((always_inline)) {
-    if constexpr (I8) {
+    if constexpr (I8 && !RAW) {
 #pragma unroll
       for (int pass = 0; pass < NPASS; ++pass) sav[i & 1][pass] = sc.row[min(rbase + i * 32 + pass * RPP + lane / LPR, M - 1)];
     }
   };
-  if constexpr (I8) {
+  if constexpr (I8 && !RAW) {
     const int oc = (lane % LPR) * V;
     const int col = EPI == 2 ? cbase + oc / 32 * 64 + oc % 32 : cbase + oc;
 #pragma unroll
@@ -468,7 +469,12 @@ __global__ __launch_bounds__(256) void gemm_tile_kernel(const bf16_t* __restrict
 #pragma unroll
     for (int j = 0; j < QN; ++j)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) stg[(8 * (r >> 2) + 4 * h + (r & 3)) * ROWF + j * 32 + r32] = (float)acc[i][j][r];
+      for (int r = 0; r < 16; ++r) {
+        float& at = stg[(8 * (r >> 2) + 4 * h + (r & 3)) * ROWF + j * 32 + r32];
+        const auto sum = acc[i][j][r];  // a copy: a bit cast of a vector's element reads its first
+        if constexpr (RAW) at = __builtin_bit_cast(float, sum);
+        else at = (float)sum;
+      }
     // LDS accesses of one wave complete in order: the reads below see the writes
 #pragma unroll
     for (int pass = 0; pass < NPASS; ++pass) {
@@ -500,7 +506,7 @@ __global__ __launch_bounds__(256) void gemm_tile_kernel(const bf16_t* __restrict
           v[e + 2] = a4.z;
           v[e + 3] = a4.w;
         }
-        if constexpr (I8) {
+        if constexpr (I8 && !RAW) {
 #pragma unroll
           for (int e = 0; e < V; ++e) v[e] *= sav[i & 1][pass] * swv[0][e];
         }
@@ -560,14 +566,14 @@ int launch_tile_g(int M, int N, int cols, int K, const void* A, const void* W, c
 // The int8 form; N may end inside the last tile.
 template <int QM, int QN, int NS, bool NT, int EPI, typename TR, typename TC>
 int launch_tile_i8(int M, int N, int cols, int K, const void* A, const float* sa, const void* W, const float* sw,
-                   const void* R, void* C, hipStream_t st, int group) {
+                   const void* R, void* C, hipStream_t st, int splits, int group) {
   using G = tile::Geo<QM, QN, NS>;
   static const hipError_t attr = hipFuncSetAttribute((const void*)gemm_tile_kernel<int8_t, QM, QN, NS, NT, EPI, TR, TC>,
                                                      hipFuncAttributeMaxDynamicSharedMemorySize, (int)G::LDS_BYTES);
   if (attr != hipSuccess) return -1;
   const int tiles_m = (M + G::BM - 1) / G::BM, tiles_n = (cols + G::BN - 1) / G::BN;
-  hipLaunchKernelGGL((gemm_tile_kernel<int8_t, QM, QN, NS, NT, EPI, TR, TC>), dim3(tiles_m * tiles_n), dim3(tile::NT),
-                     G::LDS_BYTES, st, (const bf16_t*)A, (const bf16_t*)W, (const TR*)R, (TC*)C, M, N, K, tiles_n, group, 1,
+  hipLaunchKernelGGL((gemm_tile_kernel<int8_t, QM, QN, NS, NT, EPI, TR, TC>), dim3(tiles_m * tiles_n * splits), dim3(tile::NT),
+                     G::LDS_BYTES, st, (const bf16_t*)A, (const bf16_t*)W, (const TR*)R, (TC*)C, M, N, K, tiles_n, group, splits,
                      I8Scales{sa, sw});
   return 0;
 }
@@ -632,7 +638,7 @@ int tile_group(int M, int N, int qm);
 // layer's products have it.
 #define PS_I8_INSTANCES_NT(X, QM, QN, NS, NT)                                                                \
   X(QM, QN, NS, NT, 0, float, bf16_t) X(QM, QN, NS, NT, 0, float, float) X(QM, QN, NS, NT, 1, bf16_t, float) \
-  X(QM, QN, NS, NT, 1, float, bf16_t) X(QM, QN, NS, NT, 1, bf16_t, bf16_t)
+  X(QM, QN, NS, NT, 1, float, bf16_t) X(QM, QN, NS, NT, 1, bf16_t, bf16_t) X(QM, QN, NS, NT, 0, float, int)
 #define PS_I8_INSTANCES_ALL(X, QM, QN, NS) \
   PS_I8_INSTANCES_NT(X, QM, QN, NS, false) PS_I8_INSTANCES_NT(X, QM, QN, NS, true)
 #define PS_I8_INSTANCES_256(X)                                                      \
@@ -652,6 +658,6 @@ int tile_group(int M, int N, int qm);
 #define PS_I8_INSTANTIATE(QM, QN, NS, NT, EPI, TR, TC)                                                          \
   template int launch_tile_i8<QM, QN, NS, NT, EPI, TR, TC>(int, int, int, int, const void*, const float*,       \
                                                            const void*, const float*, const void*, void*,      \
-                                                           hipStream_t, int);
+                                                           hipStream_t, int, int);
 
 }  // namespace ps

@@ -13,7 +13,7 @@ namespace ps {
 #define PS_I8_EXTERN(QM, QN, NS, NT, EPI, TR, TC)                                                                 \
   extern template int launch_tile_i8<QM, QN, NS, NT, EPI, TR, TC>(int, int, int, int, const void*, const float*,  \
                                                                   const void*, const float*, const void*, void*, \
-                                                                  hipStream_t, int);
+                                                                  hipStream_t, int, int);
 PS_I8_INSTANCES(PS_I8_EXTERN)
 #undef PS_I8_EXTERN
 
@@ -32,56 +32,7 @@ struct Args {
 
 int pad(int x, int to) { return (x + to - 1) / to * to; }
 
-// ---------------------------------------------------------------- tiles, M > 64
-template <int EPI, typename TR, typename TC>
-constexpr bool kAllShapes = !(EPI != 0 && std::is_same<TR, float>::value && std::is_same<TC, float>::value);
-
-template <int EPI, typename TR, typename TC>
-int tile_cols(const Args& x, int cols, TilePlan pl) {
-  const int group = tile_group(x.M, cols, kTileCfgs[pl.cfg].qm);
-  const bool nt = tile_nt(x.M, kTileCfgs[pl.cfg]);
-#define PS_I8_GO(QM, QN, NS, NT) \
-  launch_tile_i8<QM, QN, NS, NT, EPI, TR, TC>(x.M, x.N, cols, x.K, x.a, x.sa, x.w, x.sw, x.r, x.c, x.st, group)
-#define PS_I8_GO_NT(QM, QN, NS) (nt ? PS_I8_GO(QM, QN, NS, true) : PS_I8_GO(QM, QN, NS, false))
-  if constexpr (kAllShapes<EPI, TR, TC>) {
-    switch (pl.cfg) {
-      case 0: return PS_I8_GO_NT(4, 4, 2);
-      case 1: return PS_I8_GO_NT(3, 4, 2);
-      case 2: return PS_I8_GO_NT(2, 4, 3);
-      case 3: return PS_I8_GO_NT(4, 2, 3);
-      case 4: return PS_I8_GO_NT(3, 2, 3);
-      case 5: return PS_I8_GO_NT(2, 2, 4);
-      default: break;
-    }
-    if constexpr (EPI != 2) {
-      if (pl.cfg == 6) return PS_I8_GO_NT(2, 1, 6);
-      if (pl.cfg == 7) return PS_I8_GO(1, 1, 5, false);  // M > 64: two tile rows at least
-    }
-    return -1;
-  } else {
-    return PS_I8_GO(4, 4, 2, false);
-  }
-#undef PS_I8_GO_NT
-#undef PS_I8_GO
-}
-
-template <int EPI, typename TR, typename TC>
-int launch_tiles(const Args& x) {
-  const int kp = pad(x.K, tile::BK);
-  const TilePlan pl = gemm_tile_plan(x.M, pad(x.N, 256), kp, 1, EPI == 2);
-  TilePlan first, rest;
-  const int n = kAllShapes<EPI, TR, TC> && x.N % 256 == 0 ? tile_columns(x.M, x.N, kp, EPI == 2, pl, &first, &rest) : 0;
-  if (n == 0) return tile_cols<EPI, TR, TC>(x, x.N, pl);
-  if (tile_cols<EPI, TR, TC>(x, n, first)) return -1;
-  Args y = x;
-  y.w = (const bf16_t*)x.w + (long)(n / 64) * (kp / 64) * kWTileElts;
-  y.sw = x.sw + n;
-  y.r = x.r ? (const TR*)x.r + n : nullptr;
-  y.c = (TC*)x.c + (EPI == 2 ? n / 2 : n);
-  return tile_cols<EPI, TR, TC>(y, x.N - n, rest);
-}
-
-// --------------------------------------------------------------- skinny, M <= 64
+// ------------------------------------------------------------ K splits
 // Sums the splits' int32 partials and applies scales and epilogue, four columns
 // per thread.
 template <int EPI, typename TR, typename TC>
@@ -123,6 +74,84 @@ __global__ __launch_bounds__(256) void gemm_i8_reduce_kernel(const int* __restri
   }
 }
 
+template <int EPI, typename TR, typename TC>
+void reduce(const Args& x, int splits, const int* part) {
+  const long n4 = (long)x.M * (EPI == 2 ? x.N / 2 : x.N) / 4;
+  hipLaunchKernelGGL((gemm_i8_reduce_kernel<EPI, TR, TC>), dim3((int)std::min<long>((n4 + 255) / 256, 4096)), dim3(256), 0,
+                     x.st, part, (const TR*)x.r, (TC*)x.c, x.M, x.N, splits, x.sa, x.sw);
+}
+
+// ---------------------------------------------------------------- tiles, M > 64
+template <int EPI, typename TR, typename TC>
+constexpr bool kAllShapes = !(EPI != 0 && std::is_same<TR, float>::value && std::is_same<TC, float>::value);
+
+template <int EPI, typename TR, typename TC>
+int tile_cols(const Args& x, int cols, TilePlan pl) {
+  const int group = tile_group(x.M, cols, kTileCfgs[pl.cfg].qm);
+  const bool nt = tile_nt(x.M, kTileCfgs[pl.cfg]);
+#define PS_I8_GO(QM, QN, NS, NT) \
+  launch_tile_i8<QM, QN, NS, NT, EPI, TR, TC>(x.M, x.N, cols, x.K, x.a, x.sa, x.w, x.sw, x.r, x.c, x.st, pl.s, group)
+#define PS_I8_GO_NT(QM, QN, NS) (nt ? PS_I8_GO(QM, QN, NS, true) : PS_I8_GO(QM, QN, NS, false))
+  if constexpr (kAllShapes<EPI, TR, TC>) {
+    switch (pl.cfg) {
+      case 0: return PS_I8_GO_NT(4, 4, 2);
+      case 1: return PS_I8_GO_NT(3, 4, 2);
+      case 2: return PS_I8_GO_NT(2, 4, 3);
+      case 3: return PS_I8_GO_NT(4, 2, 3);
+      case 4: return PS_I8_GO_NT(3, 2, 3);
+      case 5: return PS_I8_GO_NT(2, 2, 4);
+      default: break;
+    }
+    if constexpr (EPI != 2) {
+      if (pl.cfg == 6) return PS_I8_GO_NT(2, 1, 6);
+      if (pl.cfg == 7) return PS_I8_GO(1, 1, 5, false);  // M > 64: two tile rows at least
+    }
+    return -1;
+  } else {
+    return PS_I8_GO(4, 4, 2, false);
+  }
+#undef PS_I8_GO_NT
+#undef PS_I8_GO
+}
+
+// Tile shape, and K splits where by the bf16 cost model they save more than the 4 us
+// of a reduction's launch (us, whole -> split and reduced, weights cold: 65 x 2048 x
+// 16384 26.9 -> 16.3, 128 x 4096 x 14336 35.8 -> 23.6, 256 x 8192 x 28672 97.6 ->
+// 72.4, 768 x 4096 x 14336 66.3 -> 56.4; 200 x 4096 x 14336 28.1 -> 28.8. Left whole:
+// 256 x 10240 x 8192 41.8, split 45.0; 128 x 4096 x 4096 10.3 and 11.0).
+TilePlan tile_plan(int M, int N, int K, bool swiglu) {  // K in pairs
+  const int kp = pad(K, tile::BK), np = pad(N, 256);
+  double whole, split;
+  const TilePlan s = gemm_tile_plan(M, np, kp, 4, false, &split);
+  const TilePlan w = gemm_tile_plan(M, np, kp, 1, false, &whole);
+  if (s.s > 1 && split + 4.0 < whole) return s;
+  return swiglu ? gemm_tile_plan(M, np, kp, 1, true) : w;
+}
+
+template <int EPI, typename TR, typename TC>
+int launch_tiles(const Args& x, int* part) {
+  const int kp = pad(x.K, tile::BK);
+  const TilePlan pl = tile_plan(x.M, x.N, x.K, EPI == 2);
+  if (pl.s > 1) {
+    Args p = x;
+    p.r = nullptr, p.c = part;
+    if (tile_cols<0, float, int>(p, x.N, pl)) return -1;
+    reduce<EPI, TR, TC>(x, pl.s, part);
+    return 0;
+  }
+  TilePlan first, rest;
+  const int n = kAllShapes<EPI, TR, TC> && x.N % 256 == 0 ? tile_columns(x.M, x.N, kp, EPI == 2, pl, &first, &rest) : 0;
+  if (n == 0) return tile_cols<EPI, TR, TC>(x, x.N, pl);
+  if (tile_cols<EPI, TR, TC>(x, n, first)) return -1;
+  Args y = x;
+  y.w = (const bf16_t*)x.w + (long)(n / 64) * (kp / 64) * kWTileElts;
+  y.sw = x.sw + n;
+  y.r = x.r ? (const TR*)x.r + n : nullptr;
+  y.c = (TC*)x.c + (EPI == 2 ? n / 2 : n);
+  return tile_cols<EPI, TR, TC>(y, x.N - n, rest);
+}
+
+// --------------------------------------------------------------- skinny, M <= 64
 template <int MB, int WN, int EPI, typename TR, typename TC, bool DIRECT>
 int skinny_k(const Args& x, int S, int* part) {
   constexpr size_t lds = skinny::lds_bytes<MB, WN>();
@@ -147,15 +176,31 @@ int skinny_mb(const Args& x, SkinnyPlan pl, int* part) {
   if (pl.wn == 2 ? skinny_k<MB, 2, EPI == 2 ? 2 : 0, float, float, false>(x, pl.s, part)
                  : skinny_k<MB, 1, 0, float, float, false>(x, pl.s, part))
     return -1;
-  const long n4 = (long)x.M * (EPI == 2 ? x.N / 2 : x.N) / 4;
-  hipLaunchKernelGGL((gemm_i8_reduce_kernel<EPI, TR, TC>), dim3((int)std::min<long>((n4 + 255) / 256, 4096)), dim3(256), 0,
-                     x.st, part, (const TR*)x.r, (TC*)x.c, x.M, x.N, pl.s, x.sa, x.sw);
+  reduce<EPI, TR, TC>(x, pl.s, part);
   return 0;
+}
+
+// The bf16 plan for half the K, except that K splits of one weight block per
+// workgroup are taken where they make as many workgroups (256 at most, of at least
+// eight stages) with fewer splits, or more: half the bytes leave the partial sums
+// twice the share (us, product and reduction, two blocks -> one: 64 x 4096 x 14336
+// 19.1 -> 17.0, 64 x 8192 x 8192 20.3 -> 18.5, 1 row 15.2 -> 14.0, 64 x 4096 x 4096
+// 10.8 -> 10.4). Long K at many rows stays with two, which read the activations half
+// as often (64 x 8192 x 28672 42.6, with one 44.9; at 16 rows 39.3 and 38.6).
+SkinnyPlan skinny_plan(int M, int N, int K) {  // K in pairs
+  const int stages = pad(K, skinny::KS) / skinny::KS;
+  const SkinnyPlan p = gemm_skinny_plan(M, N, stages * skinny::KS);
+  if (p.s == 1 && p.wn > 1) return p;
+  const int blocks = N / 64;
+  const int s = std::max(1, std::min({8, 256 / blocks, stages / 8}));
+  const int wgs = blocks * s, had = blocks / p.wn * p.s;
+  if (wgs > had || (wgs == had && s < p.s && (M <= 32 || K <= 8192))) return {1, s};
+  return p;
 }
 
 template <int EPI, typename TR, typename TC>
 int launch_skinny(const Args& x, int* part) {
-  const SkinnyPlan pl = gemm_skinny_plan(x.M, x.N, pad(x.K, skinny::KS));
+  const SkinnyPlan pl = skinny_plan(x.M, x.N, x.K);
   switch ((x.M + 15) / 16) {
     case 1: return skinny_mb<1, EPI, TR, TC>(x, pl, part);
     case 2: return skinny_mb<2, EPI, TR, TC>(x, pl, part);
@@ -172,8 +217,9 @@ int gemm_i8_check(int epi, int M, int N, int K) {
 }
 
 size_t gemm_i8_workspace_bytes(int M, int N, int K) {
-  if (M <= 0 || M > skinny::MAXM || gemm_i8_check(0, M, N, K)) return 0;
-  return (size_t)gemm_skinny_plan(M, N, pad(K / 2, skinny::KS)).s * M * N * sizeof(int);
+  if (M <= 0 || gemm_i8_check(0, M, N, K)) return 0;
+  const int s = M <= skinny::MAXM ? skinny_plan(M, N, K / 2).s : tile_plan(M, N, K / 2, false).s;
+  return M > skinny::MAXM && s == 1 ? 0 : (size_t)s * M * N * sizeof(int);
 }
 
 int launch_gemm_i8(int r_dt, int c_dt, int epi, int M, int N, int K, const void* A, const float* a_scale, const void* W,
@@ -183,7 +229,7 @@ int launch_gemm_i8(int r_dt, int c_dt, int epi, int M, int N, int K, const void*
   const Args x{M, N, K / 2, A, a_scale, W, w_scale, R, C, st};
 #define PS_I8_CASE(E, TR, TC, rd, cd) \
   if (epi == E && (E != 1 || r_dt == rd) && c_dt == cd) \
-    return M <= skinny::MAXM ? launch_skinny<E, TR, TC>(x, (int*)ws) : launch_tiles<E, TR, TC>(x);
+    return M <= skinny::MAXM ? launch_skinny<E, TR, TC>(x, (int*)ws) : launch_tiles<E, TR, TC>(x, (int*)ws);
   PS_I8_CASE(0, float, bf16_t, 0, 1)
   PS_I8_CASE(0, float, float, 0, 0)
   PS_I8_CASE(1, bf16_t, float, 1, 0)
