@@ -151,6 +151,122 @@ int launch_tiles(const Args& x, int* part) {
   return tile_cols<EPI, TR, TC>(y, x.N - n, rest);
 }
 
+// ------------------------------------------------------- narrow, M <= 16
+// Latency counts here: one launch, nothing through memory. A workgroup owns 16 CB
+// output columns over all of K; its eight waves take the W tiles (2 KiB of each
+// per 16 rows) in turn, straight into registers, two tiles in flight behind the
+// two that are multiplied, and their int32 sums meet in LDS. SwiGLU: 16 CB gate
+// columns and the up columns beside them.
+namespace narrow {
+constexpr int NW = 8, U = 2, MAXM = 16;  // waves; tiles of a wave per step
+
+// W rows per workgroup in blocks of 16: the fewest that leave no compute unit a
+// second workgroup; 0 where a workgroup would have more than 128 KiB of W to read
+// alone (96 past eight rows, which it also has to gather), and the splits are
+// faster (us, skinny -> narrow at 1 and 16 rows: 2048 x 2048 6.1 -> 3.7, 6.3 -> 4.6;
+// 4096 x 4096 7.5 -> 5.8, 8.4 -> 7.1; 8192 x 2048 6.9 -> 5.3, 7.8 -> 6.2; 6144 x 4096
+// 8.5 -> 8.1, 8.9 and 9.6; 2048 x 8192 8.2 -> 8.5, 9.6 and 11.0, of which a launch
+// more is not seen in a stream that waits for the host; left to the splits: 4096 x
+// 14336 13.0 and 13.6, 10240 x 8192 16.7 and 25.4).
+int blocks(int M, int N, int K, bool swiglu) {
+  int nb = swiglu ? 2 : 1;
+  while (nb < (swiglu ? 4 : 2) && N / (16 * nb) > compute_units()) nb *= 2;
+  return M <= MAXM && N / (16 * nb) <= compute_units() && (long)nb * K <= (M <= 8 ? 8192 : 6144) ? nb : 0;
+}
+}  // namespace narrow
+
+template <int CB, int EPI, typename TR, typename TC>
+__global__ __launch_bounds__(64 * narrow::NW) void gemm_i8_narrow_kernel(const int8_t* __restrict__ A,
+                                                                         const int8_t* __restrict__ W,
+                                                                         const TR* __restrict__ R, TC* __restrict__ C, int M,
+                                                                         int N, int K, const float* __restrict__ sa,
+                                                                         const float* __restrict__ sw) {
+  using namespace narrow;
+  using Op = Operand<int8_t>;
+  constexpr int PAIR = EPI == 2 ? 2 : 1, NB = PAIR * CB, WT = 2 * kWTileElts;  // bytes of a W tile
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  __shared__ int s_sum[NW][NB][MAXM * 16];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int g = lane >> 4, c = lane & 15;
+  const int KT = (K + 127) / 128;
+  const int j0 = blockIdx.x * (16 * CB);  // first output column, and its row of W
+  const int n0 = EPI == 2 ? j0 / kGateUpBlock * (2 * kGateUpBlock) + j0 % kGateUpBlock : j0;
+  auto wrow = [](int b) { return 16 * (b % CB) + kGateUpBlock * (b / CB); };  // of block b: gate blocks, then up
+  const int8_t* wp = W + (long)(n0 >> 6) * KT * WT + ((n0 & 63) + c) * 128 + 16 * g;
+  const int8_t* ap = A + (long)min(c, M - 1) * K;
+  struct Tiles {
+    u32x4 w[U][NB][2], a[U][2];
+  };
+  auto load = [&](int t0) __attribute__((always_inline)) {
+    Tiles x;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int t = min(t0 + NW * u, KT - 1);  // past the last: that one again, not used
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+          x.w[u][b][j] = __builtin_nontemporal_load((const u32x4*)(wp + (long)t * WT + wrow(b) * 128 + 64 * j));
+        // W is zero where K ends inside a tile
+        x.a[u][j] = *(const u32x4*)(ap + min(t * 128 + 64 * j + 16 * g, K - 16));
+      }
+    }
+    return x;
+  };
+  typename Op::Acc4 acc[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) acc[b] = typename Op::Acc4{0, 0, 0, 0};
+  auto products = [&](const Tiles& x, int t0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (t0 + NW * u >= KT) return;
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+          acc[b] = Op::mfma16(__builtin_bit_cast(Op::Frag, x.a[u][j]), __builtin_bit_cast(Op::Frag, x.w[u][b][j]), acc[b]);
+    }
+  };
+  Tiles x = load(wave), y;
+  for (int t = wave; t < KT; t += 2 * NW * U) {
+    if (t + NW * U < KT) y = load(t + NW * U);
+    products(x, t);
+    if (t + NW * U >= KT) break;
+    if (t + 2 * NW * U < KT) x = load(t + 2 * NW * U);
+    products(y, t + NW * U);
+  }
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) s_sum[wave][b][(4 * g + r) * 16 + c] = acc[b][r];
+  __syncthreads();
+  for (int e = threadIdx.x; e < MAXM * 16 * CB; e += 64 * NW) {
+    const int cc = e & 15, cb = (e >> 4) % CB, row = e / (16 * CB);
+    if (row >= M) break;
+    float v[PAIR];
+#pragma unroll
+    for (int p = 0; p < PAIR; ++p) {
+      const int b = CB * p + cb;
+      int sum = 0;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) sum += s_sum[w][b][row * 16 + cc];
+      v[p] = (float)sum * (sa[row] * sw[n0 + wrow(b) + cc]);
+    }
+    const long idx = (long)row * (N / PAIR) + j0 + 16 * cb + cc;
+    if constexpr (EPI == 2) v[0] = silu_fast(v[0]) * v[1];
+    if constexpr (EPI == 1) v[0] += ld_elt<TR>(R, idx);
+    st_elt<TC>(C, idx, v[0]);
+  }
+}
+
+template <int CB, int EPI, typename TR, typename TC>
+int launch_narrow(const Args& x) {
+  hipLaunchKernelGGL((gemm_i8_narrow_kernel<CB, EPI, TR, TC>), dim3((EPI == 2 ? x.N / 2 : x.N) / (16 * CB)),
+                     dim3(64 * narrow::NW), 0, x.st, (const int8_t*)x.a, (const int8_t*)x.w, (const TR*)x.r, (TC*)x.c, x.M,
+                     x.N, 2 * x.K, x.sa, x.sw);
+  return 0;
+}
+
 // --------------------------------------------------------------- skinny, M <= 64
 template <int MB, int WN, int EPI, typename TR, typename TC, bool DIRECT>
 int skinny_k(const Args& x, int S, int* part) {
@@ -199,7 +315,9 @@ SkinnyPlan skinny_plan(int M, int N, int K) {  // K in pairs
 }
 
 template <int EPI, typename TR, typename TC>
-int launch_skinny(const Args& x, int* part) {
+int launch_few(const Args& x, int* part) {
+  if (const int nb = narrow::blocks(x.M, x.N, 2 * x.K, EPI == 2))
+    return nb == (EPI == 2 ? 2 : 1) ? launch_narrow<1, EPI, TR, TC>(x) : launch_narrow<2, EPI, TR, TC>(x);
   const SkinnyPlan pl = skinny_plan(x.M, x.N, x.K);
   switch ((x.M + 15) / 16) {
     case 1: return skinny_mb<1, EPI, TR, TC>(x, pl, part);
@@ -229,7 +347,7 @@ int launch_gemm_i8(int r_dt, int c_dt, int epi, int M, int N, int K, const void*
   const Args x{M, N, K / 2, A, a_scale, W, w_scale, R, C, st};
 #define PS_I8_CASE(E, TR, TC, rd, cd) \
   if (epi == E && (E != 1 || r_dt == rd) && c_dt == cd) \
-    return M <= skinny::MAXM ? launch_skinny<E, TR, TC>(x, (int*)ws) : launch_tiles<E, TR, TC>(x, (int*)ws);
+    return M <= skinny::MAXM ? launch_few<E, TR, TC>(x, (int*)ws) : launch_tiles<E, TR, TC>(x, (int*)ws);
   PS_I8_CASE(0, float, bf16_t, 0, 1)
   PS_I8_CASE(0, float, float, 0, 0)
   PS_I8_CASE(1, bf16_t, float, 1, 0)

@@ -146,7 +146,8 @@ SHAPES = [(1, 64, 64), (1, 6144, 4096), (5, 128, 192), (16, 320, 4160), (17, 64,
           (65, 64, 64), (100, 192, 320), (130, 320, 1088), (389, 1024, 512), (257, 4096, 1024), (300, 576, 4096),
           (1000, 2048, 192), (700, 28672, 256), (2500, 512, 704),
           (2600, 8192, 512), (4400, 6208, 768), (4400, 6208, 640),  # several rounds of 256x256 tiles, and of two launches
-          (97, 320, 16448), (300, 576, 14400), (130, 1024, 9280)]  # K splits of tiles
+          (97, 320, 16448), (300, 576, 14400), (130, 1024, 9280),  # K splits of tiles
+          (2, 6208, 4032), (9, 4096, 1088), (16, 8192, 1536), (7, 2048, 8192), (8, 16384, 1984), (3, 192, 3200)]  # narrow
 
 
 @pytest.mark.parametrize("M,N,K", SHAPES)
