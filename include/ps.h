@@ -554,7 +554,8 @@ ps_status ps_op_gemm_i8(int32_t r_dtype, int32_t c_dtype, int32_t epilogue, int3
 /* RoPE + paged KV write for `layer`: qkv [rows, d_q + 2 d_kv] (cfg.dtype)
  * holds the QKV projection of rows grouped by sequence as in ps_prefill;
  * writes rotated q to q_out [rows, d_q] and rotated k and v into the pages
- * at positions [len, len + n_tok). */
+ * at positions [len, len + n_tok). On an e4m3 pool a call that touches at most
+ * 128 pages leaves ws unwritten (it has to be there all the same). */
 ps_status ps_op_rope_kvwrite(ps_kv* kv, int32_t layer, int32_t n_seqs, const int32_t* seqs,
                              const int32_t* n_tok, const void* qkv, void* q_out, void* ws,
                              size_t ws_bytes, void* stream);
@@ -565,7 +566,9 @@ ps_status ps_op_rope_kvwrite(ps_kv* kv, int32_t layer, int32_t n_seqs, const int
  * o [rows, n_q * hd]. Uses the prefill kernel. Few rows behind long prefixes
  * are walked by several workgroups each as far as ws has room for their
  * partial results beside the call's metadata; so the order of a row's sums,
- * and with it the rounding, depends on ws_bytes. */
+ * and with it the rounding, depends on ws_bytes (and on the other sequences of
+ * the call). On an e4m3 pool a small call (16 sequences, 384 pages, 128 tiles of
+ * 32 rows) that is not cut leaves ws unwritten. */
 ps_status ps_op_attention(ps_kv* kv, int32_t layer, int32_t n_seqs, const int32_t* seqs,
                           const int32_t* n_tok, const void* q, void* o, void* ws, size_t ws_bytes,
                           void* stream);
@@ -580,7 +583,9 @@ ps_status ps_op_attention(ps_kv* kv, int32_t layer, int32_t n_seqs, const int32_
  * then, or a batch that alone exceeds 1024 workgroups); else the smallest
  * multiple of 4 pages, at least 8, that keeps the workgroups (splits times KV
  * heads) within about 1024, two full rounds of the chip, or 16 pages where
- * the fewer splits are estimated to be faster.
+ * the fewer splits are estimated to be faster. For an e4m3 pool: of 8, 16, 32 ..
+ * 256 pages, whole sequences and lengths half-way between the one estimated to be
+ * fastest, of at least 8 pages and at most 16 workgroups per compute unit.
  * PS_E_UNSUPPORTED when the splits come to more than 65535
  * work items (one grid row each). */
 ps_status ps_op_decode_attention(ps_kv* kv, int32_t layer, int32_t n_seqs, const int32_t* seqs,
@@ -605,7 +610,8 @@ ps_status ps_op_decode_run(ps_kv* kv, int32_t layer, const void* q, void* o, voi
                            void* stream);
 
 /* ps_op_decode_run with the attention launch capped at max_workgroups
- * workgroups (rounded down to a multiple of n_kv_heads, at least n_kv_heads):
+ * workgroups (rounded down to a multiple of n_kv_heads, at least n_kv_heads; on an
+ * e4m3 pool, n_kv_heads for every 16 query heads of a KV head or part of 16):
  * each workgroup then walks several split items in turn, the form the mixed
  * step uses beside its prefill GEMMs. Same bits as the uncapped run (each
  * item's arithmetic does not depend on which workgroup runs it).

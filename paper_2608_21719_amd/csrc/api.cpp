@@ -947,6 +947,7 @@ PrefillSplit plan_prefill_ranges(const std::vector<SeqInfo>& si, size_t count, i
     }
   if (longest < 2 * kMin) return best;
   const int max_parts = max_parts_of();
+  if (max_parts < 2) return best;
   const int fill = std::min(3, std::max(1, ((int)t.size() * groups + compute_units() - 1) / compute_units()));
   // with three on a unit the longest walk runs beside shorter ones that end before it
   const double walk = fill < 3 ? longest : 0.5 * (longest + (double)total / t.size());
@@ -958,7 +959,8 @@ PrefillSplit plan_prefill_ranges(const std::vector<SeqInfo>& si, size_t count, i
     PrefillSplit p;
     long load, most;  // key tiles of the open range, and of the fullest
     int items, most_items;
-    for (;; target += std::max<long>(1, target / 32)) {  // until the ranges are n at most and the parts fit the room
+    // until the ranges are n at most and the parts fit the room
+    for (;; target += std::max<long>(1, target / (p.n_parts > max_parts ? 4 : 32))) {
       p = PrefillSplit{};
       load = most = 0, items = 0, most_items = 1;
       auto close = [&] {
