@@ -917,24 +917,24 @@ PrefillSplit plan_prefill_split(const std::vector<SeqInfo>& si, size_t count, in
 // The e4m3 kernel's split: the query tiles' walks laid end to end and cut into
 // equal ranges, one workgroup each (and KV head), so that every one ends at the
 // same time whatever the lengths; a range that ends inside a walk leaves a part.
-// For one, two and three workgroups per compute unit; the cheapest of them and
-// the whole walks is taken. Costs in us, measured: a key tile takes kTile[r] with r
-// workgroups on a unit, an item kItem beside its tiles, the merge as above. Whole
-// walks -> ranges, 8B heads: 64 rows behind 16000 tokens 353 -> 52, 512 behind 4000
-// 100 -> 68, 1024 behind 8000 211 -> 176, 445, 365 and 426 behind 7000 235 -> 179, 9
-// behind 1500 37 -> 22; 2048 behind 8000 (325) and more stay whole (3071 cut into
-// ranges 465 -> 517).
+// For one and two workgroups per compute unit (as many as fit); the cheapest of
+// them and the whole walks is taken. Costs in us, measured: a key tile takes kTile[r]
+// with r workgroups on a unit, an item kItem beside its tiles, the merge as above.
+// Whole walks -> ranges, 8B heads: 64 rows behind 16000 tokens 287 -> 43, 512 behind
+// 4000 83 -> 60, 445, 365 and 426 behind 7000 212 -> 181, 9 behind 1500 33 -> 20; 1024
+// behind 8000 (170, in ranges 169 to 184), 2048 behind 8000 (317, 333 to 364) and
+// three of 512 behind 1000 (51, 63) stay whole.
 template <typename MaxParts>
 PrefillSplit plan_prefill_ranges(const std::vector<SeqInfo>& si, size_t count, int groups, int n_q, MaxParts&& max_parts_of) {
   PrefillSplit best;
   const int qt = fa_query_tile(), kt = fa_key_tile();
-  constexpr double kTile[4] = {0, 0.72, 1.03, 1.55}, kItem = 3.0;
+  constexpr double kTile[3] = {0, 0.60, 1.05}, kItem = 3.0;
   constexpr int kMin = 12;  // key tiles of an item that is cut
   struct Tile {
     int32_t b, q0, tiles;
   };
   std::vector<Tile> t;
-  const int slots = 3 * compute_units() / std::max(1, groups);
+  const int slots = 2 * compute_units() / std::max(1, groups);
   long total = 0;
   int longest = 0;
   for (size_t b = 0; b < count; ++b)
@@ -948,11 +948,9 @@ PrefillSplit plan_prefill_ranges(const std::vector<SeqInfo>& si, size_t count, i
   if (longest < 2 * kMin) return best;
   const int max_parts = max_parts_of();
   if (max_parts < 2) return best;
-  const int fill = std::min(3, std::max(1, ((int)t.size() * groups + compute_units() - 1) / compute_units()));
-  // with three on a unit the longest walk runs beside shorter ones that end before it
-  const double walk = fill < 3 ? longest : 0.5 * (longest + (double)total / t.size());
-  double cost = 0.95 * (walk * kTile[fill] + kItem);  // a split has to promise a twentieth
-  for (int r = 1; r <= 3; ++r) {
+  const int fill = (int)t.size() * groups > compute_units() ? 2 : 1;
+  double cost = 0.95 * (longest * kTile[fill] + kItem);  // a split has to promise a twentieth
+  for (int r = 1; r <= 2; ++r) {
     const int n = r * compute_units() / std::max(1, groups);  // ranges
     if (n < 1) continue;
     long target = std::max<long>((total + n - 1) / n, kMin);

@@ -297,9 +297,16 @@ int launch_kv8_decode(int G, int hd, int n_items, int n_kv, int n_seqs, const vo
 // A tile's bytes go through registers: waves 0, 2 widen the keys of its pages,
 // waves 1, 3 the values, once for all four heads: 16 conversions and eight 8-byte
 // LDS stores per lane and tile, the same instructions for keys and values (only the
-// lane's LDS offsets differ), so that they run between the products of the tile
-// before. The bytes are requested two tiles before that, their page ids one more:
-// a walk alone on its compute unit waits for nothing but its own arithmetic.
+// lane's LDS offsets differ), set between the products Q K of the tile before. The
+// bytes are requested two tiles before that, their page ids one more.
+//
+// A walk is a chain of LDS reads, products and exponentials. At two waves per SIMD
+// (209 registers) the reads leave it: a tile's K operands are all read at its head,
+// its V operands before the exponentials. Against three waves of 168 registers, with
+// operands read one or two ahead: 0.57 us a tile instead of 0.69 for a walk alone,
+// 1024 rows 27.3 -> 24.4 us, three of 512 behind 1000 to 7000 tokens 183 -> 170, 8 x
+// 2048 301 -> 308 (0.89 PFLOP/s, at the 1400 W cap either way: two workgroups on a
+// compute unit take 1.05 us for a tile of each, three 1.55).
 // LDS, two slots: K row = key, 16-byte chunk p of row r holds dims of chunk p ^
 // (r % 16) (hd 64: of 8 chunks, r % 8). V^T per page: row = dim, 16 tokens with
 // the quads in the order 0 2 1 3, which is how P lies in a lane (k = 8 g + e: token
@@ -325,7 +332,7 @@ struct NoPrefillMeta {};
 // query tiles; parts leave O unnormalised with their base and sum for the merge.
 enum class Fa { kWhole, kInline, kSplit };
 template <int HD, Fa F>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void kv8_prefill_kernel(
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void kv8_prefill_kernel(
     typename std::conditional<F == Fa::kInline, Kv8PrefillMeta, NoPrefillMeta>::type, const bf16_t* __restrict__ q, Kv8Layer kv,
     const SeqInfo* __restrict__ si, const int32_t* __restrict__ bt,
     const typename std::conditional<F == Fa::kSplit, PrefillSplitItem, PrefillItem>::type* __restrict__ items,
@@ -335,6 +342,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k
   constexpr int KE = kPageTokens * HD;  // elements of a page's keys
   constexpr int TILE = KT * HD * 2;  // bytes of a tile's keys; its values follow
   __shared__ __attribute__((aligned(1024))) char s_kv[2][2 * TILE];
+  // A masked weight is 0, but 0 x NaN is not. In tiles that some row does not see to
+  // their end, NaN values are stored as 0, and each dim's first position of one is
+  // kept: the rows from it on are NaN there. Two sets, by the item's parity.
+  __shared__ int s_first[2][HD], s_any[2];
   const int hq = (G + 3) / 4;
   const int kvh = blockIdx.y / hq;
   const int n_q = n_kv * G;
@@ -365,7 +376,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k
   const int kv_valid = s.kv_before + s.n_new;
   int kt0 = 0, n_tiles = (qpos0 + qn + KT - 1) / KT;
   if constexpr (SPLIT) kt0 = it.kt_begin, n_tiles = it.kt_end;
-  const float2* scales = kv.scales + (long)kvh * kv.n_pages;
+  // a scale is read as a vector: the wait for a scalar load would hold the LDS reads up
+  const __amdgpu_buffer_rsrc_t scales = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<float2*>(kv.scales) + (long)kvh * kv.n_pages, (short)0, kv.n_pages * (int)sizeof(float2), 0x00020000);
+
+  int(&first_nan)[HD] = s_first[item & 1];
+  int& any_nan = s_any[item & 1];
+  if (threadIdx.x < HD) first_nan[threadIdx.x] = INT32_MAX;
+  if (threadIdx.x == 0) any_nan = 0;
 
   // this wave's half of one page of a tile
   const int pg = wave >> 1;
@@ -381,7 +399,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k
   auto fetch = [&](int page) __attribute__((always_inline)) {
     Raw r;
     const uint8_t* base = kv.blocks + kv8_block(page, kvh, n_kv, HD) + (values ? KE : 0) + lane * 16;
-    r.s = values ? scales[page].y : scales[page].x;
+    r.s = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(scales, page * 8 + (values ? 4 : 0), 0, 0));
 #pragma unroll
     for (int i = 0; i < NB; ++i) r.w[i] = *(const uint4*)(base + 1024 * i);
     return r;
@@ -396,13 +414,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k
       at[i][j] = values ? TILE + pg * KE * 2 + dim * 32 + (((lq & 1) ^ ((dim >> 3) & 1)) << 4) + ((lq >> 1) << 3)
                         : (16 * pg + lc) * HD * 2 + ((ch ^ (lc & (CH - 1))) << 4) + ((j & 1) << 3);
     }
-  auto put = [&](Raw r, int kt, char* slot) __attribute__((always_inline)) {
-    const int valid = kv_valid - (2 * kt + pg) * kPageTokens;
-    if (valid < kPageTokens && values) {  // slots that hold no token may hold any byte: zero, so that 0 x NaN does not arise
-      const uint32_t keep = token_bytes(valid - 4 * lq);
-#pragma unroll
-      for (int i = 0; i < NB; ++i) r.w[i] = make_uint4(r.w[i].x & keep, r.w[i].y & keep, r.w[i].z & keep, r.w[i].w & keep);
-    }
+  auto put = [&](const Raw& r, char* slot) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
       const uint32_t w[4] = {r.w[i].x, r.w[i].y, r.w[i].z, r.w[i].w};
@@ -410,6 +422,33 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k
       for (int j = 0; j < 4; ++j)
         *(uint2*)(slot + at[i][j]) = make_uint2(e4m3_bf2<false>(w[j], r.s), e4m3_bf2<true>(w[j], r.s));
     }
+  };
+
+  // For a tile that some row does not see to its end, after put by the same wave:
+  // value slots that hold no token may hold any byte: zero, as NaN is (first_nan).
+  // In LDS, as registers that a branch may change are copied, which waits for them.
+  auto scrub = [&](int kt, char* slot) __attribute__((always_inline)) {
+    if (!values || kt >= n_tiles || kt * KT + KT - 1 <= qpos0) return;
+    const int pos = (2 * kt + pg) * kPageTokens + 4 * lq;  // of the quad's first token
+    const uint32_t keep = token_bytes(kv_valid - pos);
+    auto halves = [](uint32_t two) { return (two & 0xff) * 0x101u | (two >> 8 & 0xff) * 0x1010000u; };
+    auto nan = [](uint32_t w) {
+      return ((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+    };
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        uint2* p = (uint2*)(slot + at[i][j]);
+        uint2 w = *p;
+        w = make_uint2(w.x & halves(keep), w.y & halves(keep >> 16));
+        const uint32_t nx = nan(w.x), ny = nan(w.y);
+        if (nx | ny) {
+          atomicMin(&first_nan[64 * i + 16 * j + lc], pos + (nx & 0xffff ? 0 : nx ? 1 : ny & 0xffff ? 2 : 3));
+          any_nan = 1;
+        }
+        *p = make_uint2(w.x & ~nx, w.y & ~ny);
+      }
   };
 
   bf16x8_t qf[KK];
@@ -435,28 +474,43 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k
   int id = page_id(kt0 + 2);
   raw[0] = fetch(page_id(kt0));
   raw[1] = fetch(page_id(kt0 + 1));
-  put(raw[0], kt0, s_kv[0]);
+  kv8_lds_barrier();  // first_nan
+  put(raw[0], s_kv[0]);
+  scrub(kt0, s_kv[0]);
   raw[0] = fetch(id);
   id = page_id(kt0 + 3);
   kv8_lds_barrier();
 
-  auto tile = [&](int kt, auto slotc, auto firstc) __attribute__((always_inline)) {
-    constexpr bool FIRST = decltype(firstc)::value;
+  auto tile = [&](int kt, auto slotc, auto firstc, auto diagc) __attribute__((always_inline)) {
+    constexpr bool FIRST = decltype(firstc)::value, DIAG = decltype(diagc)::value;  // DIAG: some row may not see all of it
     constexpr int SLOT = decltype(slotc)::value;
     const int k0 = kt * KT;
     const char *K = s_kv[SLOT], *V = s_kv[SLOT] + TILE;
-    put(raw[SLOT ^ 1], kt + 1, s_kv[SLOT ^ 1]);  // past the walk's end: never read
+    bf16x8_t kf[KK];
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) kf[kk] = __builtin_bit_cast(bf16x8_t, *(const uint4*)(K + (kread ^ (32 * kk))));
+    __builtin_amdgcn_sched_barrier(0);  // the reads stay ahead of the stores
+    put(raw[SLOT ^ 1], s_kv[SLOT ^ 1]);  // past the walk's end: never read
     raw[SLOT ^ 1] = fetch(id);
-    id = page_id(kt + 4);
     f32x16_t sacc;
 #pragma unroll
     for (int r = 0; r < 16; ++r) sacc[r] = 0.f;
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
-      const bf16x8_t a = __builtin_bit_cast(bf16x8_t, *(const uint4*)(K + (kread ^ (32 * kk))));
-      sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[kk], sacc, 0, 0, 0);
+    for (int kk = 0; kk < KK; ++kk) sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kk], qf[kk], sacc, 0, 0, 0);
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {  // a product, four vector instructions, an LDS store
+      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x2, 4, 0);
+      __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
     }
-    if (k0 + KT - 1 > qpos0) {
+    bf16x8_t vf[2][DB];
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+      for (int db = 0; db < DB; ++db) vf[p][db] = __builtin_bit_cast(bf16x8_t, *(const uint4*)(V + p * KE * 2 + db * 32 * 32 + vread));
+    __builtin_amdgcn_sched_barrier(0);
+    id = page_id(kt + 4);  // a scalar load: awaited with the V operands, behind the exponentials
+    if (DIAG && k0 + KT - 1 > qpos0) {
 #pragma unroll
       for (int r = 0; r < 16; ++r)
         if (k0 + 8 * (r >> 2) + 4 * g + (r & 3) > qpos) sacc[r] = -INFINITY;
@@ -514,22 +568,34 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k
       const bf16x8_t bp = __builtin_bit_cast(bf16x8_t, make_uint4(pk[4 * p], pk[4 * p + 1], pk[4 * p + 2], pk[4 * p + 3]));
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
-        const bf16x8_t a = __builtin_bit_cast(bf16x8_t, *(const uint4*)(V + p * KE * 2 + db * 32 * 32 + vread));
-        oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, bp, oacc[db], 0, 0, 0);
+        oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[p][db], bp, oacc[db], 0, 0, 0);
       }
     }
+    if constexpr (DIAG) scrub(kt + 1, s_kv[SLOT ^ 1]);
     kv8_lds_barrier();  // the next tile is written; every wave is done with this one
   };
   using Even = std::integral_constant<int, 0>;
   using Odd = std::integral_constant<int, 1>;
-  tile(kt0, Even{}, std::true_type{});
-  for (int kt = kt0 + 1; kt < n_tiles; kt += 2) {
-    tile(kt, Odd{}, std::false_type{});
-    if (kt + 1 < n_tiles) tile(kt + 1, Even{}, std::false_type{});
+  tile(kt0, Even{}, std::true_type{}, std::true_type{});
+  int kt = kt0 + 1;
+  for (; kt + 2 < n_tiles && (kt + 3) * KT - 1 <= qpos0; kt += 2) {  // tiles to kt + 2 are seen whole by every row
+    tile(kt, Odd{}, std::false_type{}, std::false_type{});
+    tile(kt + 1, Even{}, std::false_type{}, std::false_type{});
+  }
+  for (; kt < n_tiles; kt += 2) {
+    tile(kt, Odd{}, std::false_type{}, std::true_type{});
+    if (kt + 1 < n_tiles) tile(kt + 1, Even{}, std::false_type{}, std::true_type{});
   }
 
   const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(lsum), __float_as_uint(lsum), false, false);
   const float l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+  if (any_nan) {
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (qpos >= first_nan[32 * db + 8 * (r >> 2) + 4 * g + (r & 3)]) oacc[db][r] = __uint_as_float(0x7fc00000u);
+  }
   if (!live || c >= qn) continue;
   if constexpr (SPLIT) {
     if (it.part >= 0) {

@@ -386,6 +386,35 @@ def test_non_finite_keys_reach_only_the_rows_that_see_them():
     assert np.isnan(got[40:60]).all() and np.isfinite(got[:40]).all() and np.isfinite(got[60:]).all()
 
 
+@pytest.mark.parametrize("hd,past,bad", [(128, 0, (40, 7)), (64, 0, (31, 63)), (128, 21, (0, 127)), (128, 16, (33, 64))])
+def test_non_finite_values_reach_only_the_rows_that_see_them(hd, past, bad):
+    """An infinity among the values, in the same tile as rows before it; earlier calls' tokens are finite."""
+    rng = np.random.default_rng(18)
+    n, (at, dim) = 70, bad
+    p = Pool8(shape(4, 1, hd), 32)
+    k, v = wide(bf16(rng, (past + n, 1, hd))).astype(np.float32), wide(bf16(rng, (past + n, 1, hd))).astype(np.float32)
+    outs = []
+    for x in (0.0, np.inf, -np.inf, np.nan):
+        v[past + at, 0, dim] = x
+        s, = p.seqs([past + n])
+        kb, vb = gen.to_storage(k, "bf16"), gen.to_storage(v, "bf16")
+        if past:
+            p.append([s], [past], kb[:past], vb[:past])
+        p.append([s], [n], kb[past:], vb[past:])
+        p.kv.truncate(s, past)
+        q = H.to_dev(bf16(np.random.default_rng(19), (n, 4, hd)), "bf16")
+        o = H.empty((n, 4 * hd), "bf16")
+        B.op_attention(p.kv, 0, [s], [n], q, o, p.ws)
+        torch.cuda.synchronize()
+        outs.append(H.to_f64(o).reshape(n, 4, hd))
+        p.kv.free(s)
+    clean = outs[0]
+    for got in outs[1:]:
+        assert np.isnan(got[at:, :, dim]).all()
+        assert np.isfinite(got[:at]).all() and np.array_equal(got[:at], clean[:at])
+        assert np.array_equal(np.delete(got, dim, 2), np.delete(clean, dim, 2))
+
+
 def test_results_repeat_bit_for_bit():
     rng = np.random.default_rng(17)
     p, seqs, kv = filled(shape(32, 8, 128), [4000, 50], [1, 1], rng)
