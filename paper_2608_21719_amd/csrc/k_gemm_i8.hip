@@ -2,10 +2,17 @@
 // sums, a scale for each row of A (token) and each row of W (output channel). The
 // sums are exact (K < 2^17), so a result does not depend on tile shapes or splits.
 //
-// The kernels are the bf16 GEMMs' with int8 operands (Operand<int8_t>): W lies in
-// 64 x 128 tiles of the same 8 KiB, an MFMA takes the same 16 bytes per lane for
-// twice the k. So a launch costs what a bf16 launch of half the K costs, and the
-// plans (tile shape, weight blocks, K splits) are taken for that.
+// Tiles (M > 64) and skinny (M <= 64) are the bf16 GEMMs' kernels with int8 operands
+// (Operand<int8_t>): W lies in 64 x 128 tiles of the same 8 KiB, an MFMA takes the
+// same 16 bytes per lane for twice the k. So a launch costs what a bf16 launch of
+// half the K costs, and the plans (tile shape, weight blocks, K splits) start from
+// that. Up to 16 rows have a kernel of their own where W is small (narrow).
+//
+// Reached: 16384 x 28672 x 4096 (SwiGLU) 1.52 ms, 2.5 POP/s, at the 1400 W cap's 1.8
+// GHz (the MFMA alone reaches 3.2 to 3.5 POP/s on random operands); 389 x 8192 x 8192
+// 36 us, where a 128 x 128 tile's LDS traffic (64 KB read, 32 filled a stage) takes
+// longer than its MFMAs; up to 64 rows the weight stream, 64 x 4096 x 14336 at 3.5 TB/s,
+// 64 x 57344 x 8192 at 6.4 TB/s.
 #include "gemm_skinny.h"
 
 namespace ps {
