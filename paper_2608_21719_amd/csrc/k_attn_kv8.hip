@@ -306,8 +306,8 @@ int launch_kv8_decode(int G, int hd, int n_items, int n_kv, int n_seqs, const vo
 // (209 registers) the reads leave it: a tile's K operands are all read at its head,
 // its V operands before the exponentials. Against three waves of 168 registers, with
 // operands read one or two ahead: 0.57 us a tile instead of 0.69 for a walk alone,
-// 1024 rows 27.3 -> 24.4 us, three of 512 behind 1000 to 7000 tokens 183 -> 170, 8 x
-// 2048 301 -> 308 (0.89 PFLOP/s, at the 1400 W cap either way: two workgroups on a
+// 1024 rows 27.3 -> 24.4 us, three of 300 to 512 behind 6000 to 12000 tokens 183 ->
+// 170, 8 x 2048 301 -> 308 (0.89 PFLOP/s, at the 1400 W cap either way: two workgroups on a
 // compute unit take 1.05 us for a tile of each, three 1.55).
 // LDS, two slots: K row = key, 16-byte chunk p of row r holds dims of chunk p ^
 // (r % 16) (hd 64: of 8 chunks, r % 8). V^T per page: row = dim, 16 tokens with
