@@ -2203,7 +2203,7 @@ extern "C" ps_status ps_op_gemm_i8(int32_t r_dt, int32_t c_dt, int32_t epi, int3
   const size_t need = gemm_i8_workspace_bytes(M, N, K);
   if (need && (!ws || ws_bytes < need)) return fail(PS_E_INVALID, "workspace too small for split-K partials");
   if (M == 0) return PS_OK;
-  if (launch_gemm_i8(r_dt, c_dt, epi, M, N, K, A, a_scale, Wt, w_scale, R, C, ws, ws_bytes, (hipStream_t)stream))
+  if (launch_gemm_i8(r_dt, c_dt, epi, M, N, K, A, a_scale, Wt, w_scale, R, C, ws, (hipStream_t)stream))
     return fail(PS_E_UNSUPPORTED, "dtype/epilogue combination not supported");
   return last_launch_error();
   PS_CATCH

@@ -130,9 +130,13 @@ TilePlan tile_plan(int M, int N, int K, bool swiglu) {  // K in pairs
   const int kp = pad(K, tile::BK), np = pad(N, 256);
   double whole, split;
   const TilePlan s = gemm_tile_plan(M, np, kp, 4, false, &split);
-  const TilePlan w = gemm_tile_plan(M, np, kp, 1, false, &whole);
-  if (s.s > 1 && split + 4.0 < whole) return s;
-  return swiglu ? gemm_tile_plan(M, np, kp, 1, true) : w;
+  if (s.s == 1 && !swiglu) return s;
+  if (s.s > 1) {
+    const TilePlan w = gemm_tile_plan(M, np, kp, 1, false, &whole);
+    if (split + 4.0 < whole) return s;
+    if (!swiglu) return w;
+  }
+  return gemm_tile_plan(M, np, kp, 1, true);
 }
 
 template <int EPI, typename TR, typename TC>
@@ -348,9 +352,9 @@ size_t gemm_i8_workspace_bytes(int M, int N, int K) {
 }
 
 int launch_gemm_i8(int r_dt, int c_dt, int epi, int M, int N, int K, const void* A, const float* a_scale, const void* W,
-                   const float* w_scale, const void* R, void* C, void* ws, size_t ws_bytes, hipStream_t st) {
+                   const float* w_scale, const void* R, void* C, void* ws, hipStream_t st) {
   if (M == 0) return 0;
-  if (gemm_i8_check(epi, M, N, K) || ws_bytes < gemm_i8_workspace_bytes(M, N, K)) return -1;
+  if (gemm_i8_check(epi, M, N, K)) return -1;
   const Args x{M, N, K / 2, A, a_scale, W, w_scale, R, C, st};
 #define PS_I8_CASE(E, TR, TC, rd, cd) \
   if (epi == E && (E != 1 || r_dt == rd) && c_dt == cd) \

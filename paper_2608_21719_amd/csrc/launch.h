@@ -204,11 +204,11 @@ hipError_t gemm_static_scratch(void** out);
 // Rows to int8 with a scale each; g not null: their RMSNorm with that gain.
 int launch_quant_rows(int x_dt, int g_dt, int rows, int d, const void* x, const void* g, float eps, void* q, float* scale,
                       hipStream_t st);
-// C = epi(a_scale w_scale A W^T), int8 operands; ws: int32 partials.
+// C = epi(a_scale w_scale A W^T), int8 operands; ws: gemm_i8_workspace_bytes for int32 partials.
 int gemm_i8_check(int epi, int M, int N, int K);  // 0: supported
 size_t gemm_i8_workspace_bytes(int M, int N, int K);
 int launch_gemm_i8(int r_dt, int c_dt, int epi, int M, int N, int K, const void* A, const float* a_scale, const void* W,
-                   const float* w_scale, const void* R, void* C, void* ws, size_t ws_bytes, hipStream_t st);
+                   const float* w_scale, const void* R, void* C, void* ws, hipStream_t st);
 
 // model-level kernels (bf16 rows)
 // One metadata upload: n16 16-byte units from mapped host memory (src) to
