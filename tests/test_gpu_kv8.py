@@ -426,3 +426,111 @@ def test_results_repeat_bit_for_bit():
         torch.cuda.synchronize()
         outs.append(H.bits(o))
     assert all(np.array_equal(x, outs[0]) for x in outs[1:])
+
+
+def test_writes_of_128_and_of_more_pages_are_the_same():
+    """A call's work list as a kernel argument or through the workspace: the same bytes and rows."""
+    rng = np.random.default_rng(20)
+    n = 129 * PAGE
+    p = Pool8(shape(4, 2, 64), 4 * 130, max_pages=129)
+    qkv = H.to_dev(bf16(rng, (n, 8, 64)), "bf16")
+    got = []
+    for calls in ([n], [n - PAGE, PAGE], [PAGE, n - PAGE]):
+        s, = p.seqs([n])
+        q = H.empty((n, 4, 64), "bf16")
+        r0 = 0
+        for t in calls:
+            B.op_rope_kvwrite(p.kv, 0, [s], [t], qkv[r0:], q[r0:], p.ws)
+            p.kv.commit([s], [t])
+            r0 += t
+        torch.cuda.synchronize()
+        got.append((H.to_f64(q), *p.gather(s)))
+    for other in got[1:]:
+        assert all(np.array_equal(a, b) for a, b in zip(got[0], other))
+    # many sequences: 129 one-page prompts against one at a time
+    seqs = Pool8(shape(4, 2, 64), 260, max_seqs=130, max_pages=1)
+    one = seqs.seqs([PAGE] * 129)
+    q = H.empty((n, 4, 64), "bf16")
+    B.op_rope_kvwrite(seqs.kv, 0, one, [PAGE] * 129, qkv, q, seqs.ws)
+    seqs.kv.commit(one, [PAGE] * 129)
+    for i in (0, 63, 128):
+        s, = p.seqs([PAGE])
+        alone = H.empty((PAGE, 4, 64), "bf16")
+        B.op_rope_kvwrite(p.kv, 0, [s], [PAGE], qkv[i * PAGE:], alone, p.ws)
+        p.kv.commit([s], [PAGE])
+        torch.cuda.synchronize()
+        assert np.array_equal(H.bits(q)[i * PAGE:(i + 1) * PAGE], H.bits(alone))
+        assert all(np.array_equal(a, b) for a, b in zip(seqs.gather(one[i]), p.gather(s)))
+
+
+@pytest.mark.parametrize("new", [[5] * 16, [5] * 17, [40, 3] * 10, [128 * 32], [128 * 32 + 1], [700] * 9])
+def test_prefill_work_lists_of_either_kind_give_the_same_bits(new):
+    """Rows of a sequence do not depend on which others share the call, nor on how the work list travels."""
+    rng = np.random.default_rng(21)
+    p, seqs, _ = filled(shape(2, 1, 64), [0] * len(new), new, rng)
+    rows = sum(new)
+    q = H.to_dev(bf16(rng, (rows, 2, 64)), "bf16")
+    small = H.workspace(32768)  # no room for parts: whole walks
+    together, alone = H.empty((rows, 128), "bf16"), H.empty((rows, 128), "bf16")
+    B.op_attention(p.kv, 0, seqs, new, q, together, small)
+    r0 = 0
+    for s, n in zip(seqs, new):
+        for c0 in range(0, n, 2048):  # chunks of whole tiles
+            n_c = min(2048, n - c0)
+            B.op_attention(p.kv, 0, [s], [n_c], q[r0 + c0:], alone[r0 + c0:], small)
+            p.kv.commit([s], [n_c])
+        r0 += n
+    torch.cuda.synchronize()
+    assert np.array_equal(H.bits(together), H.bits(alone))
+
+
+@pytest.mark.parametrize("at", [0, 13, 36])
+def test_non_finite_values_in_split_walks(at):
+    rng = np.random.default_rng(22)
+    past, n = 6000, 37
+    p = Pool8(shape(4, 1, 128, ffn=28672), 2 * 380, max_pages=380, rows=6100)
+    k, v = (wide(bf16(rng, (past + n, 1, 128))).astype(np.float32) for _ in range(2))
+    v[past + at, 0, 100] = np.inf
+    s, = p.seqs([past + n])
+    p.append([s], [past], *(gen.to_storage(x[:past], "bf16") for x in (k, v)))
+    p.append([s], [n], *(gen.to_storage(x[past:], "bf16") for x in (k, v)))
+    p.kv.truncate(s, past)
+    q = H.to_dev(bf16(rng, (n, 4, 128)), "bf16")
+    for ws in (p.ws, H.workspace(16384)):
+        o = H.empty((n, 512), "bf16")
+        B.op_attention(p.kv, 0, [s], [n], q, o, ws)
+        torch.cuda.synchronize()
+        bad = np.isnan(H.to_f64(o).reshape(n, 4, 128))
+        want = np.zeros_like(bad)
+        want[at:, :, 100] = True
+        assert np.array_equal(bad, want)
+
+
+def test_a_pool_past_four_gib():
+    """Pages whose bytes lie past 32-bit offsets: written, gathered, read by both attentions, copied."""
+    rng = np.random.default_rng(23)
+    n = 2000
+    p = Pool8(shape(2, 1, 128), 1_300_000, max_seqs=2, max_pages=130, rows=2048)
+    s, = p.seqs([n])
+    assert max(p.kv.block_table(s)) * 4096 > 2 ** 32
+    k, v = bf16(rng, (n, 1, 128)), bf16(rng, (n, 1, 128))
+    p.append([s], [n], k, v)
+    ref = [K.Sequence(1, 128) for _ in range(2)]
+    for r, x in zip(ref, (k, v)):
+        r.append(wide(x))
+    got = p.gather(s)
+    assert all(np.array_equal(a, r.values()) for a, r in zip(got, ref))
+    t = Pool8(shape(2, 1, 128), 130, max_seqs=2, max_pages=130)
+    d, = t.seqs([n])
+    B.kv_transfer(p.kv, s, t.kv, d, t.ws)
+    assert all(np.array_equal(a, b) for a, b in zip(t.gather(d), got))
+    p.kv.truncate(s, n - 40)
+    q = bf16(rng, (40, 2, 128))
+    o = H.empty((40, 256), "bf16")
+    B.op_attention(p.kv, 0, [s], [40], H.to_dev(q, "bf16"), o, p.ws)
+    torch.cuda.synchronize()
+    check(H.to_f64(o).reshape(40, 2, 128), wide(q), *got, np.arange(n - 40, n), "prefill")
+    p.kv.truncate(s, n - 41)
+    B.op_decode_attention(p.kv, 0, [s], H.to_dev(q[:1], "bf16"), o[:1], p.ws)
+    torch.cuda.synchronize()
+    check(H.to_f64(o[:1]).reshape(1, 2, 128), wide(q[:1]), got[0][:n - 40], got[1][:n - 40], np.array([n - 41]), "decode")
