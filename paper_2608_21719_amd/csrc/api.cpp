@@ -920,8 +920,8 @@ PrefillSplit plan_prefill_split(const std::vector<SeqInfo>& si, size_t count, in
 // For one and two workgroups per compute unit (as many as fit); the cheapest of
 // them and the whole walks is taken. Costs in us, measured: a key tile takes kTile[r]
 // with r workgroups on a unit, an item kItem beside its tiles, the merge as above.
-// Whole walks -> ranges, 8B heads: 64 rows behind 16000 tokens 287 -> 43, 512 behind
-// 4000 83 -> 60, 445, 365 and 426 behind 7000 212 -> 181, 9 behind 1500 33 -> 20; 1024
+// Whole walks -> ranges, 8B heads: 64 rows behind 16000 tokens 287 -> 40, 512 behind
+// 4000 83 -> 60, 445, 365 and 426 behind 7000 212 -> 181, 9 behind 1500 33 -> 19; 1024
 // behind 8000 (170, in ranges 169 to 184), 2048 behind 8000 (317, 333 to 364) and
 // three of 512 behind 1000 (51, 63) stay whole.
 template <typename MaxParts>

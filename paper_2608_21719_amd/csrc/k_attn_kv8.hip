@@ -635,15 +635,34 @@ __global__ __launch_bounds__(256) void kv8_merge_kernel(const PrefillMerge* __re
   if (c >= mg.n_rows || head >= n_q) return;
   const float* ml = parts.ml + (((long)mg.part * n_q + head) * kPT + c) * 2;
   const long step = (long)n_q * kPT * 2;
+  // four parts at a time: with many, the time is the loads' latency (16 parts 42.7 -> 39.9 us with the attention)
   float M = -INFINITY;
-  for (int p = 0; p < mg.n_parts; ++p) M = fmaxf(M, ml[p * step]);
-  float x[W] = {}, L = 0.f;
-  for (int p = 0; p < mg.n_parts; ++p) {
-    const float* po = parts.part(mg.part + p, (long)n_q * kPT * HD) + ((long)head * kPT + c) * HD + W * lane;
-    const float f = ml[p * step] == -INFINITY ? 0.f : exp2f(ml[p * step] - M);
+  for (int p = 0; p < mg.n_parts; p += 4) {
+    float b[4];
 #pragma unroll
-    for (int i = 0; i < W; ++i) x[i] += po[i] * f;
-    L += ml[p * step + 1] * f;
+    for (int u = 0; u < 4; ++u) b[u] = ml[min(p + u, mg.n_parts - 1) * step];
+    M = fmaxf(M, fmaxf(fmaxf(b[0], b[1]), fmaxf(b[2], b[3])));
+  }
+  float x[W] = {}, L = 0.f;
+  for (int p = 0; p < mg.n_parts; p += 4) {
+    float v[4][W];
+    float2 s[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int at = min(p + u, mg.n_parts - 1);
+      const float* po = parts.part(mg.part + at, (long)n_q * kPT * HD) + ((long)head * kPT + c) * HD + W * lane;
+#pragma unroll
+      for (int i = 0; i < W; ++i) v[u][i] = po[i];
+      s[u] = *(const float2*)(ml + at * step);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (p + u >= mg.n_parts) break;
+      const float f = s[u].x == -INFINITY ? 0.f : exp2f(s[u].x - M);
+#pragma unroll
+      for (int i = 0; i < W; ++i) x[i] += v[u][i] * f;
+      L += s[u].y * f;
+    }
   }
   bf16_t* op = o + ((long)(mg.row + c) * n_q + head) * HD + W * lane;
 #pragma unroll
