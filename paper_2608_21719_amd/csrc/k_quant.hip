@@ -62,6 +62,19 @@ struct Quant {
   }
 };
 
+// The mean square plus eps of a row of ordinary values; else its squares pass the
+// range of fp32 or fall out of it, and the row is taken times 2^-norm_exp.
+__device__ __forceinline__ bool norm_in_range(float ms) { return ms >= 0x1p-100f && ms < INFINITY; }
+// Exponent of the larger of max |x| (by its bits) and sqrt(eps), so that the
+// scaled squares and eps sum to 1/4 at least and about 4 d at most; 0 for an
+// infinity or NaN, which no scaling saves.
+__device__ __forceinline__ int norm_exp(uint32_t bits, float eps) {
+  if (bits >= 0x7f800000u) return 0;
+  int e = bits ? ilogbf(__uint_as_float(bits)) : -149;
+  if (eps > 0.f) e = max(e, ilogbf(eps) / 2);
+  return e;
+}
+
 __device__ __forceinline__ uint32_t pack4(int a, int b, int c, int d) {
   return (uint32_t)(a & 255) | (uint32_t)(b & 255) << 8 | (uint32_t)(c & 255) << 16 | (uint32_t)d << 24;
 }
@@ -100,7 +113,25 @@ __global__ __launch_bounds__(NT) void quant_rows_kernel(const TX* __restrict__ x
     }
   }
   if constexpr (NORM) {
-    const float inv = 1.0f / sqrtf(row_sum<NT>(ss, red) / (float)d + eps);
+    float ms = row_sum<NT>(ss, red) / (float)d + eps;
+    if (!norm_in_range(ms)) {  // the same for every thread
+      uint32_t mx = 0;
+#pragma unroll
+      for (int c = 0; c < VPT; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) mx = max(mx, __float_as_uint(v[c][e]) & 0x7fffffffu);
+      const int ex = norm_exp(row_max_bits<NT>(mx, redb), eps);
+      ss = 0.f;
+#pragma unroll
+      for (int c = 0; c < VPT; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          v[c][e] = ldexpf(v[c][e], -ex);
+          ss += v[c][e] * v[c][e];
+        }
+      ms = row_sum<NT>(ss, red) / (float)d + ldexpf(eps, -2 * ex);
+    }
+    const float inv = 1.0f / sqrtf(ms);
 #pragma unroll
     for (int c = 0; c < VPT; ++c) {
       const int i = (c * NT + threadIdx.x) * 8;
@@ -146,18 +177,29 @@ __global__ __launch_bounds__(256) void quant_rows_any_kernel(const TX* __restric
   const long row = blockIdx.x;
   const TX* xr = x + row * d;
   float inv = 1.f;
+  int ex = 0;
+  auto scaled = [&](int i) { return ldexpf(Elt<TX>::load(xr, i), -ex); };
   if constexpr (NORM) {
-    float ss = 0.f;
-    for (int i = threadIdx.x; i < d; i += 256) {
-      const float v = Elt<TX>::load(xr, i);
-      ss += v * v;
+    auto mean_square = [&] {
+      float ss = 0.f;
+      for (int i = threadIdx.x; i < d; i += 256) {
+        const float v = scaled(i);
+        ss += v * v;
+      }
+      return row_sum<256>(ss, red) / (float)d + ldexpf(eps, -2 * ex);
+    };
+    float ms = mean_square();
+    if (!norm_in_range(ms)) {
+      uint32_t mx = 0;
+      for (int i = threadIdx.x; i < d; i += 256) mx = max(mx, __float_as_uint(Elt<TX>::load(xr, i)) & 0x7fffffffu);
+      ex = norm_exp(row_max_bits<256>(mx, redb), eps);
+      ms = mean_square();
     }
-    inv = 1.0f / sqrtf(row_sum<256>(ss, red) / (float)d + eps);
+    inv = 1.0f / sqrtf(ms);
   }
   auto y = [&](int i) {
-    const float v = Elt<TX>::load(xr, i);
-    if constexpr (NORM) return v * inv * Elt<TG>::load(g, i);
-    else return v;
+    if constexpr (NORM) return scaled(i) * inv * Elt<TG>::load(g, i);
+    else return Elt<TX>::load(xr, i);
   };
   uint32_t mx = 0;
   for (int i = threadIdx.x; i < d; i += 256) mx = max(mx, __float_as_uint(y(i)) & 0x7fffffffu);
