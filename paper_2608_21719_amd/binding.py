@@ -185,11 +185,12 @@ def device_info(device: int = 0) -> dict:
 
 
 def ints(seq):
-    """int32 array argument of a sequence of integers (64 of them 1.1 us; converted one by one 7)."""
+    """int32 array argument of a sequence of numbers, as ctypes converts them (64 integers in a third of the time that
+    one by one takes)."""
     try:
-        a = array.array("i", seq)
-    except TypeError:  # numbers that are not integers: truncated
-        a = array.array("i", [int(x) for x in seq])
+        a = array.array("i", list(seq))
+    except (TypeError, OverflowError):  # not integers: truncated; past 32 bits: wrapped, for the library to refuse
+        return (c_int32 * len(seq))(*[int(x) for x in seq])
     return (c_int32 * len(a)).from_buffer(a) if a else (c_int32 * 0)()
 
 
