@@ -2,9 +2,10 @@
 // from the data sheet: HBM streaming read and copy bandwidth, the dense
 // bf16 MFMA rate of v_mfma_f32_32x32x16_bf16 on register operands (near
 // constant, and random bits changing every product, as a GEMM on real data
-// sees; also v_mfma_f32_16x16x32_bf16 on the same random data), and
+// sees; also v_mfma_f32_16x16x32_bf16 on the same random data and
+// v_mfma_i32_32x32x32_i8 on random bytes), and
 // whether MFMA and vector-ALU work issued on the same SIMD overlap in time.
-// `ceilings mfma-random [seconds [32x32x16|16x16x32]]` runs only the
+// `ceilings mfma-random [seconds [32x32x16|16x16x32|i8]]` runs only the
 // random-operand rates (or one of them) for about as long as asked, so that
 // clock and power can be sampled beside it.
 // A standalone program (not part of libps); every buffer is allocated here
@@ -28,14 +29,17 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x16 __attribute__((ext_vector_type(16)));
 
 // Random bf16 operands that change from one product to the next: each wave
 // holds 4 A and 4 B fragments of random sign and mantissa bits (exponent
 // 126 or 127, so every value is normal and no sum overflows) and pairs
 // A j with B (j + r) % 4 in rotation r. SHAPE 0: 16 v_mfma_f32_32x32x16_bf16
 // per trip over 4 accumulators; SHAPE 1: 32 v_mfma_f32_16x16x32_bf16 (the
-// same FLOPs) over 16, each reused every 16 products. One trip is 524288
-// FLOP per wave.
+// same FLOPs) over 16, each reused every 16 products; SHAPE 2: 16
+// v_mfma_i32_32x32x32_i8 on random bytes, paired as SHAPE 0. One trip is 524288
+// FLOP per wave, of SHAPE 2 twice as many operations.
 template <int SHAPE>
 __global__ __launch_bounds__(256) void mfma_random(float* out, int trips) {
   unsigned h = (blockIdx.x * 256u + threadIdx.x) * 0x9E3779B9u + 0x7F4A7C15u;
@@ -57,7 +61,25 @@ __global__ __launch_bounds__(256) void mfma_random(float* out, int trips) {
       b[j][e] = rnd_bf16();
     }
   float s = 0.f;
-  if constexpr (SHAPE == 0) {
+  if constexpr (SHAPE == 2) {
+    i32x4 a8[4], b8[4];
+    for (int j = 0; j < 4; ++j)
+      for (int e = 0; e < 4; ++e) {
+        a8[j][e] = (int)next();
+        b8[j][e] = (int)next();
+      }
+    i32x16 acc[4];
+    for (int j = 0; j < 4; ++j)
+      for (int r = 0; r < 16; ++r) acc[j][r] = 0;
+    for (int t = 0; t < trips; ++t) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(a8[j], b8[(j + r) & 3], acc[j], 0, 0, 0);
+    }
+    for (int j = 0; j < 4; ++j)
+      for (int r = 0; r < 16; ++r) s += (float)acc[j][r];
+  } else if constexpr (SHAPE == 0) {
     f32x16 acc[4];
     for (int j = 0; j < 4; ++j)
       for (int r = 0; r < 16; ++r) acc[j][r] = 0.f;
@@ -218,16 +240,17 @@ static float time_ms(hipEvent_t e0, hipEvent_t e1) {
   return ms;
 }
 
-// bf16 MFMA rate on random operands, one 4-wave workgroup per CU (one wave
+// MFMA rate on random operands, one 4-wave workgroup per CU (one wave
 // per SIMD, as the tile GEMM runs), each shape timed over about `seconds`
 static void mfma_random_rates(int cus, double seconds, hipEvent_t e0, hipEvent_t e1, int only_shape = -1) {
   float* out = nullptr;
   CHECK(hipMalloc(&out, (size_t)cus * 256 * sizeof(float)));
-  for (int shape = 0; shape < 2; ++shape) {
+  for (int shape = 0; shape < 3; ++shape) {
     if (only_shape >= 0 && shape != only_shape) continue;
     auto launch = [&](int trips) {
       if (shape == 0) hipLaunchKernelGGL(mfma_random<0>, dim3(cus), dim3(256), 0, 0, out, trips);
-      else hipLaunchKernelGGL(mfma_random<1>, dim3(cus), dim3(256), 0, 0, out, trips);
+      else if (shape == 1) hipLaunchKernelGGL(mfma_random<1>, dim3(cus), dim3(256), 0, 0, out, trips);
+      else hipLaunchKernelGGL(mfma_random<2>, dim3(cus), dim3(256), 0, 0, out, trips);
     };
     // size a launch to about 50 ms from a short one, then repeat it
     const int probe_trips = 20000;
@@ -247,9 +270,10 @@ static void mfma_random_rates(int cus, double seconds, hipEvent_t e0, hipEvent_t
     CHECK(hipGetLastError());
     float ms = 0.f;
     CHECK(hipEventElapsedTime(&ms, e0, e1));
-    const double flop = (double)cus * 4 * (double)trips * reps * 524288.0;
-    std::printf("mfma %s bf16, random operands changing every product: %.0f TFLOP/s (%.0f ms)\n",
-                shape == 0 ? "32x32x16" : "16x16x32", flop / (ms * 1e-3) / 1e12, ms);
+    const double flop = (double)cus * 4 * (double)trips * reps * 524288.0 * (shape == 2 ? 2 : 1);
+    const char* what[] = {"32x32x16 bf16", "16x16x32 bf16", "32x32x32 int8"};
+    std::printf("mfma %s, random operands changing every product: %.0f %s (%.0f ms)\n", what[shape],
+                flop / (ms * 1e-3) / 1e12, shape == 2 ? "TOP/s" : "TFLOP/s", ms);
     std::fflush(stdout);
   }
   CHECK(hipFree(out));
@@ -263,7 +287,7 @@ int main(int argc, char** argv) {
   CHECK(hipEventCreate(&e0));
   CHECK(hipEventCreate(&e1));
   if (argc > 1 && std::strcmp(argv[1], "mfma-random") == 0) {
-    const int only = argc > 3 ? (std::strcmp(argv[3], "16x16x32") == 0 ? 1 : 0) : -1;
+    const int only = argc > 3 ? (std::strcmp(argv[3], "16x16x32") == 0 ? 1 : std::strcmp(argv[3], "i8") == 0 ? 2 : 0) : -1;
     mfma_random_rates(cus, argc > 2 ? std::atof(argv[2]) : 1.0, e0, e1, only);
     return 0;
   }
