@@ -512,8 +512,8 @@ ps_status ps_op_gemm_static(int32_t dtype, int32_t r_dtype, int32_t c_dtype, int
 /* ------------------------------------------------ products in 8-bit integers
  * A linear layer as y = x W^T with x and W rounded to int8: one scale for each
  * row of x (token) and each row of W (output channel). Decode reads half the
- * weight bytes of bf16, prefill runs at twice the matrix rate (§III-B's roofline
- * terms both ways). */
+ * weight bytes of bf16, prefill runs at nearly twice the matrix rate (§III-B's
+ * roofline terms both ways). */
 
 /* q[r, :] = x[r, :] 127 / max|x[r, :]| rounded to the nearest integer (ties to
  * even), scale[r] = max|x[r, :]| / 127, so that q scale stands for x. x [rows, d]
@@ -524,12 +524,13 @@ ps_status ps_op_gemm_static(int32_t dtype, int32_t r_dtype, int32_t c_dtype, int
 ps_status ps_op_quant_rows(int32_t x_dtype, int32_t rows, int32_t d, const void* x, void* q, float* scale, void* stream);
 
 /* The same of the rows' RMSNorm, x / sqrt(mean(x^2) + eps) * g in fp32, which is
- * not rounded in between. g [d] of g_dtype. */
+ * not rounded in between; rows whose squares pass the range of fp32 are scaled by
+ * a power of two first. g [d] of g_dtype. */
 ps_status ps_op_rmsnorm_quant(int32_t x_dtype, int32_t g_dtype, int32_t rows, int32_t d, const void* x, const void* g,
                               float eps, void* q, float* scale, void* stream);
 
 /* int8 weights are stored in tiles of 64 x 128, padded with zeros: W[n, k] is at
- *   ((n / 64) * ceil(in / 128) + k / 128) * 8192 + (n % 64) * 128 + k % 128.
+ *   ((n / 64) * ceil(K / 128) + k / 128) * 8192 + (n % 64) * 128 + k % 128.
  * ps_tiled_weight_i8_bytes: bytes of the tiled form (0 for sizes refused).
  * ps_tile_weight_i8 (host) and ps_op_tile_weight_i8 (device, enqueued on stream)
  * convert a row-major int8 [N, K]; K a multiple of 64 (else PS_E_UNSUPPORTED). */
@@ -545,7 +546,10 @@ ps_status ps_op_tile_weight_i8(int32_t N, int32_t K, const void* w, void* out, v
  * when the dtypes match. N and K multiples of 64, K < 131072 (the sums then fit),
  * any M; ws of ps_op_gemm_i8_workspace_bytes (which may be 0) holds the partial
  * sums of products split over K. The result does not depend on how the product is
- * cut up: calls repeat bit for bit. */
+ * cut up: calls repeat bit for bit, and so does a row whatever rows share its
+ * call. An fp32 residual into fp32 and SwiGLU into fp32 are no layer's products:
+ * above 64 rows, unless K is split, they run on 256 x 256 tiles alone, whatever
+ * part of them M fills (4096 x 4096 at 65 rows 38 us, with a bf16 residual 10). */
 size_t ps_op_gemm_i8_workspace_bytes(int32_t M, int32_t N, int32_t K);
 ps_status ps_op_gemm_i8(int32_t r_dtype, int32_t c_dtype, int32_t epilogue, int32_t M, int32_t N, int32_t K, const void* A,
                         const float* a_scale, const void* W, const float* w_scale, const void* R, void* C, void* ws,
@@ -563,7 +567,10 @@ ps_status ps_op_rope_kvwrite(ps_kv* kv, int32_t layer, int32_t n_seqs, const int
 /* Causal attention of q [rows, n_q, hd] (rows grouped by sequence as in
  * ps_prefill, at positions [len, len + n_tok)) over the sequence's cached
  * keys 0..pos in the pages (the rows' own K/V must already be written).
- * o [rows, n_q * hd]. Uses the prefill kernel. Few rows behind long prefixes
+ * o [rows, n_q * hd]. Uses the prefill kernel. The matrix-core kernels (bf16
+ * layers of head_dim 128 with a group that is a multiple of 4, and every e4m3
+ * pool) round a row's softmax weights to bf16 for their product with the values,
+ * and sum the rounded ones. Few rows behind long prefixes
  * are walked by several workgroups each as far as ws has room for their
  * partial results beside the call's metadata; so the order of a row's sums,
  * and with it the rounding, depends on ws_bytes (and on the other sequences of
@@ -575,7 +582,8 @@ ps_status ps_op_attention(ps_kv* kv, int32_t layer, int32_t n_seqs, const int32_
 
 /* Split-K decode attention: one query row per sequence at position len
  * (the row's own K/V already written there, not yet committed), attending
- * over keys 0..len. q [n_seqs, n_q, hd], o [n_seqs, n_q * hd].
+ * over keys 0..len. q [n_seqs, n_q, hd], o [n_seqs, n_q * hd]. Softmax weights
+ * are rounded to bf16 as in ps_op_attention.
  * split_pages = at most that many pages per split: each sequence's pages
  * are cut into ceil(pages / split_pages) splits of near-equal size. 0 =
  * library choice: one split per sequence where that is estimated to be

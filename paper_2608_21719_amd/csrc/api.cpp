@@ -573,11 +573,12 @@ class DecodeCost {
   // 4 KiB page of a unit's even share (28 GB/s), 0.075 for each that the fullest unit
   // has beyond it (the others leave it bandwidth when they end), 1.0 for a round,
   // and where a sequence is split 2.4, 0.03 for each split of the longest and 0.55
-  // for each MB of partial results both ways. Fitted over 3700 batches of 1 to 160
+  // for each MB of partial results both ways. Fitted over 1170 batches of 1 to 160
   // sequences of 16 to 20000 tokens, 1 to 16 KV heads, head sizes of 64 and 128 (rms
-  // error 7%): the cheapest by this of the splits compared is 0.7% above the fastest
-  // of them on average, 5% at the 95th percentile (the 16-bit rule 5% and 26%: bytes
-  // pass twice as fast, so a split's own cost weighs twice as much).
+  // error 7%). Over 1439 others the cheapest by this of the splits compared is 1.1%
+  // above the fastest of them on average, 7% at the 95th percentile and 29% at worst
+  // (the 16-bit rule 5.7, 29 and 71%: bytes pass twice as fast, so a split's own cost
+  // weighs twice as much); heads of 64 are the weak spot, 2.5 and 16% (3.2 and 11%).
   double us8(long split, int n_q, int hd) {
     const long items = cut(split);
     long total = 0;
@@ -921,9 +922,10 @@ PrefillSplit plan_prefill_split(const std::vector<SeqInfo>& si, size_t count, in
 // them and the whole walks is taken. Costs in us, measured: a key tile takes kTile[r]
 // with r workgroups on a unit, an item kItem beside its tiles, the merge as above.
 // Whole walks -> ranges, 8B heads: 64 rows behind 16000 tokens 287 -> 40, 512 behind
-// 4000 83 -> 60, 445, 365 and 426 behind 7000 212 -> 181, 9 behind 1500 33 -> 19; 1024
-// behind 8000 (170, in ranges 169 to 184), 2048 behind 8000 (317, 333 to 364) and
-// three of 512 behind 1000 (51, 63) stay whole.
+// 4000 83 -> 61, 445, 365 and 426 behind 7000 203 -> 168, 9 behind 1500 33 -> 19, one
+// behind 30000 522 -> 43; 1024 behind 8000 (166, in ranges 169 to 184), 2048 behind
+// 8000 (301, 333 to 364) and three of 512 behind 1000 (49, 63) stay whole. Of 69 calls
+// with 32 / 8, 64 / 8 and 16 / 4 heads one is cut at a loss (1500 behind 3000, 122 -> 126).
 template <typename MaxParts>
 PrefillSplit plan_prefill_ranges(const std::vector<SeqInfo>& si, size_t count, int groups, int n_q, MaxParts&& max_parts_of) {
   PrefillSplit best;

@@ -29,7 +29,9 @@ namespace ps {
 // The pass is bound by HBM: 16 loads of 1 KiB per pair and wave, all whole
 // lines, non-temporal, two pairs in flight behind the one at work. 8B heads: 64
 // sequences of 1024 to 4096 tokens 62 us, 5.8 TB/s; 32 of 4096 to 32768 141 us with
-// the combine, 6.2 TB/s (a plain read reaches 7.1).
+// the combine, 6.2 TB/s (a plain read reaches 7.1). Groups above 16 heads read every
+// page once for each 16: 32 heads on one KV head, 128 sequences of 4096 tokens 43.9
+// us where 16 heads take 28.3 (3.05 and 4.75 TB/s of the cache).
 namespace {
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f4;
 }
@@ -292,7 +294,8 @@ int launch_kv8_decode(int G, int hd, int n_items, int n_kv, int n_seqs, const vo
 // =================================================================== prefill
 // A workgroup owns 32 query rows of one sequence and up to four query heads of
 // one KV head, a wave each (waves past the group repeat its last head and store
-// nothing), and walks 32-key tiles (two pages) up to its last row. As in the
+// nothing, so groups that are no multiple of four pay for the next one: 8 x 2048
+// rows, 32 query heads on 8, 16 and 32 KV heads 0.84, 0.49 and 0.26 PFLOP/s), and walks 32-key tiles (two pages) up to its last row. As in the
 // bf16 kernel S^T = K Q^T and O^T = V^T P^T, so that a lane holds one query
 // column of both and the statistics never cross lanes but between its halves.
 //

@@ -8,11 +8,12 @@
 // half the K costs, and the plans (tile shape, weight blocks, K splits) start from
 // that. Up to 16 rows have a kernel of their own where W is small (narrow).
 //
-// Reached: 16384 x 28672 x 4096 (SwiGLU) 1.52 ms, 2.5 POP/s, at the 1400 W cap's 1.8
-// GHz (the MFMA alone reaches 3.2 to 3.5 POP/s on random operands); 389 x 8192 x 8192
-// 36 us, where a 128 x 128 tile's LDS traffic (64 KB read, 32 filled a stage) takes
-// longer than its MFMAs; up to 64 rows the weight stream, 64 x 4096 x 14336 at 3.5 TB/s,
-// 64 x 57344 x 8192 at 6.4 TB/s.
+// Reached: 16384 x 28672 x 4096 (SwiGLU) 1.51 ms, 2.5 POP/s, at the 1400 W cap's 1.8
+// GHz (the MFMA alone reaches 3.4 POP/s on random operands); 389 x 8192 x 8192 34 us,
+// where a 128 x 128 tile's LDS traffic (64 KB read, 32 filled a stage) takes longer
+// than its MFMAs and one wave per SIMD waits for it; up to 64 rows the weight stream,
+// 64 x 4096 x 14336 at 4.1 TB/s (one weight block per workgroup, 24 KiB of weights in
+// flight per compute unit), 64 x 57344 x 8192 at 6.4 TB/s (four blocks, 64 KiB).
 #include "gemm_skinny.h"
 
 namespace ps {
