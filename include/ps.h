@@ -192,6 +192,8 @@ ps_status ps_kv_destroy(ps_kv* kv);
  * (nearest, ties to even, values past 448 2^119 to that); an infinity or NaN is
  * held as NaN. Where e grows, the earlier tokens' bytes are rounded anew to the
  * larger scale; all such roundings together stay below one step of the last. A
+ * scale that grew stays as long as the page keeps earlier tokens, also where the
+ * tokens it grew for are written anew before a commit, or truncated. A
  * page's content therefore depends on how its tokens were grouped into calls
  * only by those roundings. Keys are rotated in fp32 before they are rounded.
  * Attention reads byte * 2^e, which is exact in bf16.
